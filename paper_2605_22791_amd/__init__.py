@@ -6,6 +6,9 @@ shapes and dtypes are read from the torch tensors, outputs and workspace are
 allocated with torch when the caller does not pass them, and every step of the
 operator runs in the HIP kernels of the library on the current torch stream.
 
+Linear attention with a decay for each head (linattn.py, include/gdr2_linattn.h)
+and the block norms (blocknorm.py, include/gdr2_blocknorm.h) are called the same way.
+
 If the library is missing the functions raise; there is no fallback.
 """
 
@@ -109,6 +112,8 @@ def lib():
         L.gdr2_profile_collect.restype = ctypes.c_int
         L.gdr2_status_str.argtypes = [ctypes.c_int]
         L.gdr2_status_str.restype = ctypes.c_char_p
+        linattn._declare(L)
+        blocknorm._declare(L)
         _LIB = L
     return _LIB
 
@@ -560,3 +565,11 @@ def gdr2_fused_recurrent(q, k, v, f, a_log, delta, b, w, S, *, cu_seqlens=None, 
                                         _ptr(v), _ptr(f), _ptr(b), _ptr(w), _ptr(S), _ptr(o), _stream())
     _check(st, "gdr2_fused_recurrent")
     return o
+
+
+# --------------------------------------------------------------------------- the other operators
+from . import linattn, blocknorm  # noqa: E402  (they use the helpers above)
+from .linattn import *  # noqa: E402,F401,F403
+from .blocknorm import *  # noqa: E402,F401,F403
+
+__all__ += linattn.__all__ + blocknorm.__all__

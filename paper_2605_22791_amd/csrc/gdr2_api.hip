@@ -4,59 +4,15 @@
 
 #include "../../include/gdr2.h"
 
-#include <cmath>
 #include <type_traits>
-#include <cstdlib>
 #include <vector>
 
+#include "gdr2_host.hpp"
 #include "gdr2_kernels.hpp"
 
 using namespace gdr2;
 
 namespace {
-
-constexpr size_t kAlign = 256;
-
-size_t round_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-constexpr int kMaxSeqs = 1 << 24;  // sequences of one packed call
-
-// nseq > 0: a packed variable-length call of nseq sequences (B must be 1).
-gdr2_status check_problem(const gdr2_problem* p, bool chunked, int nseq = 0) {
-  if (p == nullptr) return GDR2_EINVAL;
-  if (p->B <= 0 || p->T <= 0 || p->H <= 0 || p->Dk <= 0 || p->Dv <= 0) return GDR2_EINVAL;
-  if (!std::isfinite(p->scale)) return GDR2_EINVAL;
-  if (p->dtype != GDR2_BF16 && p->dtype != GDR2_FP32) return GDR2_EINVAL;
-  if (nseq < 0 || (nseq > 0 && p->B != 1)) return GDR2_EINVAL;
-  if (p->Hv < 0 || (p->Hv > 0 && p->Hv % p->H != 0)) return GDR2_EINVAL;
-  if ((p->Dk != 64 && p->Dk != 128) || (p->Dv != 64 && p->Dv != 128)) return GDR2_EUNSUPPORTED;
-  if (chunked && p->chunk != CH) return GDR2_EUNSUPPORTED;
-  if (nseq > kMaxSeqs) return GDR2_EUNSUPPORTED;
-  const double Hv = p->Hv > 0 ? p->Hv : p->H;
-  const double rows = (double)p->B * (double)p->T * Hv;
-  const int dmax = p->Dk > p->Dv ? p->Dk : p->Dv;
-  if (rows * dmax >= 2147483648.0) return GDR2_EUNSUPPORTED;
-  const double states = nseq > 0 ? (double)nseq : (double)p->B;
-  if (states * Hv * (double)p->Dk * p->Dv >= 2147483648.0) return GDR2_EUNSUPPORTED;
-  return GDR2_OK;
-}
-
-// The problem seen from the value heads: every kernel runs per value head
-// (H := Hv) and reads the key-side tensors q, k, g, b at key head h / G.
-gdr2_problem value_view(const gdr2_problem* p) {
-  gdr2_problem v = *p;
-  v.H = p->Hv > 0 ? p->Hv : p->H;
-  v.Hv = 0;
-  return v;
-}
-int group_of(const gdr2_problem* p) { return p->Hv > 0 ? p->Hv / p->H : 1; }
-
-// Chunks per sequence of a fixed-length call (the last one partial when 64 does not divide T).
-int chunks_per_seq(const gdr2_problem* p) { return (p->T + CH - 1) / CH; }
-// Chunk slots of a packed call: sum_s ceil(L_s / 64) <= floor(T / 64) + nseq.
-int varlen_slots(const gdr2_problem* p, int nseq) { return p->T / CH + nseq; }
 
 // Workspace regions, chunk-head major: ch = (b*H + h)*NT + n (fixed length) or
 // h*slots + c (packed; see Varlen in gdr2_kernels.hpp).  The bf16
@@ -252,11 +208,6 @@ Layout layout(const gdr2_problem* p, bool bwd, int nseq = 0, int G = 1, bool fus
   return L;
 }
 
-template <typename T>
-T* at(void* ws, size_t off) {
-  return reinterpret_cast<T*>(static_cast<char*>(ws) + off);
-}
-
 // Everything a run needs about the chunking: the workspace layout, chunks per
 // sequence (fixed length) or chunk slots (packed), the number of scanned
 // sequences and, for packed calls, the device chunk table.
@@ -308,23 +259,6 @@ hipError_t build_table(const gdr2_problem* p, const Geo& G, hipStream_t st) {
   return launch_varlen_table(G.vl.cu, G.vl.nseq, p->T, G.vl.ncmax, const_cast<int*>(G.vl.coff),
                              const_cast<int*>(G.vl.ct0), const_cast<int*>(G.vl.clen),
                              const_cast<int*>(G.vl.sorder), st);
-}
-
-bool debug_sync() {
-  static const bool on = [] {
-    const char* e = std::getenv("GDR2_DEBUG_SYNC");
-    return e != nullptr && e[0] == '1';
-  }();
-  return on;
-}
-
-gdr2_status hip_status(hipError_t e, hipStream_t st) {
-  if (e != hipSuccess) return GDR2_EHIP;
-  if (debug_sync()) {
-    if (hipStreamSynchronize(st) != hipSuccess) return GDR2_EHIP;
-    if (hipGetLastError() != hipSuccess) return GDR2_EHIP;
-  }
-  return GDR2_OK;
 }
 
 // ---- measurement support ---------------------------------------------------

@@ -1,0 +1,497 @@
+// Linear attention with a decay for each head, chunk-parallel on fp32 matrix
+// products (v_mfma_f32_16x16x4_f32).  Three passes: every chunk's own contribution
+// to the state, the states that enter the chunks (elementwise over the chunks), and
+// the outputs of every chunk from the state that enters it.  The backward does the
+// first two for the reverse states too; its last pass has both of a chunk's
+// boundary states at hand, so that every term of the decay's gradient is a sum of
+// products and none a difference of long sums.
+//
+// The decays of a chunk are summed in 64 bits (64 values, one wave): differences of
+// sums behind a forgotten state stay exact to fp32.
+
+#include "gdr2_linattn.hpp"
+#include "gdr2_bf16.hpp"
+
+namespace gdr2 {
+
+namespace {
+
+constexpr int kThr = 256;
+
+__device__ __forceinline__ float la_in(const float* p) { return *p; }
+__device__ __forceinline__ void la_load4(const float* p, float (&x)[4]) {
+  const float4 t = ld4(p);
+  x[0] = t.x, x[1] = t.y, x[2] = t.z, x[3] = t.w;
+}
+__device__ __forceinline__ void la_load4(const bf16_t* p, float (&x)[4]) {
+  const uint2 t = *reinterpret_cast<const uint2*>(p);
+  x[0] = __uint_as_float(t.x << 16), x[1] = __uint_as_float(t.x & 0xffff0000u);
+  x[2] = __uint_as_float(t.y << 16), x[3] = __uint_as_float(t.y & 0xffff0000u);
+}
+__device__ __forceinline__ void la_put(float* p, float x) { *p = x; }
+__device__ __forceinline__ void la_put(bf16_t* p, float x) {
+  *reinterpret_cast<__bf16*>(p) = (__bf16)x;
+}
+
+// Chunk u of the flat grid: value head, chunk slot, sequence row; false past the end.
+__device__ __forceinline__ bool la_chunk(const LaGeo& a, int u, int& h, ChunkPos& p) {
+  const int x = u % a.NT, y = u / a.NT;
+  h = y % a.H;
+  return chunk_pos(a.vl, x, h, y / a.H, a.T, a.H, a.NT, p);
+}
+
+// sG[r + 1] = G_r, sG[0] = 0 (rows >= len: no decay).  One wave; the caller's barrier follows.
+__device__ __forceinline__ void la_sums(const LaGeo& a, const ChunkPos& p, int h, double* sG, int tid) {
+  if (tid < 64) {
+    double x = tid < p.len ? (double)la_decay_at(a, p.row0 + tid, h) : 0.0;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const double y = __shfl_up(x, o);
+      if (tid >= o) x += y;
+    }
+    sG[tid + 1] = x;
+    if (tid == 0) sG[0] = 0.0;
+  }
+}
+__device__ __forceinline__ float la_exp(double x) { return expf((float)x); }
+
+// 64 x D tile of one head into LDS as fp32 (row stride D + 4), rows >= len zero.
+template <int D, typename TIn>
+__device__ __forceinline__ void la_tile(const TIn* src, size_t stride, int len, float* dst, int tid) {
+  for (int e = tid; e < CH * D / 4; e += kThr) {
+    const int r = e / (D / 4), c = (e % (D / 4)) * 4;
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
+    if (r < len) la_load4(src + r * stride + c, x);
+    *reinterpret_cast<float4*>(dst + r * (D + 4) + c) = make_float4(x[0], x[1], x[2], x[3]);
+  }
+}
+
+// 16 x 16 tile  sum_c A[i0 + m][c] B[j0 + n][c]  of two LDS tiles (row stride D + 4); the
+// order of c is permuted so that a lane reads four at a time.
+template <int D>
+__device__ __forceinline__ f4 la_dot_tile(const float* A, const float* B, int i0, int j0, int lane) {
+  const float* pa = A + (i0 + (lane & 15)) * (D + 4) + 4 * (lane >> 4);
+  const float* pb = B + (j0 + (lane & 15)) * (D + 4) + 4 * (lane >> 4);
+  f4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int c = 0; c < D; c += 16) {
+    const float4 x = ld4(pa + c), y = ld4(pb + c);
+    acc = mfma4(x.x, y.x, acc);
+    acc = mfma4(x.y, y.y, acc);
+    acc = mfma4(x.z, y.z, acc);
+    acc = mfma4(x.w, y.w, acc);
+  }
+  return acc;
+}
+
+// acc[m][n] += sum_c A[i0 + m][c] S[c][n0 + n]: A in LDS (row stride D + 4), S (D x N) in memory
+template <int D, int N>
+__device__ __forceinline__ f4 la_state_tile(const float* A, const float* S, int i0, int n0, f4 acc, int lane) {
+  const float* pa = A + (i0 + (lane & 15)) * (D + 4) + 4 * (lane >> 4);
+  const float* ps = S + (size_t)(4 * (lane >> 4)) * N + n0 + (lane & 15);
+#pragma unroll 4
+  for (int c = 0; c < D; c += 16) {
+    const float4 x = ld4(pa + c);
+    acc = mfma4(x.x, ps[(c + 0) * N], acc);
+    acc = mfma4(x.y, ps[(c + 1) * N], acc);
+    acc = mfma4(x.z, ps[(c + 2) * N], acc);
+    acc = mfma4(x.w, ps[(c + 3) * N], acc);
+  }
+  return acc;
+}
+// acc[m][n] += sum_v A[i0 + m][v] S[n0 + n][v]: S (. x D) in memory, read along its rows
+template <int D>
+__device__ __forceinline__ f4 la_state_t_tile(const float* A, const float* S, int i0, int n0, f4 acc, int lane) {
+  const float* pa = A + (i0 + (lane & 15)) * (D + 4) + 4 * (lane >> 4);
+  const float* ps = S + (size_t)(n0 + (lane & 15)) * D + 4 * (lane >> 4);
+#pragma unroll 4
+  for (int v = 0; v < D; v += 16) {
+    const float4 x = ld4(pa + v), y = ld4(ps + v);
+    acc = mfma4(x.x, y.x, acc);
+    acc = mfma4(x.y, y.y, acc);
+    acc = mfma4(x.z, y.z, acc);
+    acc = mfma4(x.w, y.w, acc);
+  }
+  return acc;
+}
+
+constexpr int LP = CH + 4;  // row stride of the 64 x 64 score tile
+
+// acc[m][n] += sum_{s < 16 (i + 1)} P[16 i + m][s] Z[s][n0 + n]
+template <int D>
+__device__ __forceinline__ f4 la_rows_tile(const float* P, const float* Z, int i, int n0, f4 acc, int lane) {
+  const float* pa = P + (16 * i + (lane & 15)) * LP + 4 * (lane >> 4);
+  const float* pz = Z + 4 * (lane >> 4) * (D + 4) + n0 + (lane & 15);
+  for (int s = 0; s < 16 * (i + 1); s += 16) {
+    const float4 x = ld4(pa + s);
+    acc = mfma4(x.x, pz[(s + 0) * (D + 4)], acc);
+    acc = mfma4(x.y, pz[(s + 1) * (D + 4)], acc);
+    acc = mfma4(x.z, pz[(s + 2) * (D + 4)], acc);
+    acc = mfma4(x.w, pz[(s + 3) * (D + 4)], acc);
+  }
+  return acc;
+}
+// acc[m][n] += sum_{r >= 16 j} P[r][16 j + m] Z[r][n0 + n]
+template <int D>
+__device__ __forceinline__ f4 la_cols_tile(const float* P, const float* Z, int j, int n0, f4 acc, int lane) {
+  const int g = lane >> 4, l = lane & 15;
+  for (int r = 16 * j; r < CH; r += 4) acc = mfma4(P[(r + g) * LP + 16 * j + l], Z[(r + g) * (D + 4) + n0 + l], acc);
+  return acc;
+}
+
+}  // namespace
+
+// ---- every chunk's contribution to the state -------------------------------
+template <int DK, int DV, typename TIn, bool REV>
+__global__ __launch_bounds__(kThr) void la_state_kernel(LaStateArgs<TIn> a) {
+  __shared__ double sG[CH + 1];
+  __shared__ float sW[CH];
+  extern __shared__ __align__(16) float smem[];
+  float *sX = smem, *sZ = sX + CH * (DK + 4);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int h;
+  ChunkPos p;
+  if (!la_chunk(a.geo, blockIdx.x, h, p)) return;
+  const int HK = a.geo.H / a.geo.G, hk = h / a.geo.G;
+  la_tile<DK>(a.x + (p.row0 * HK + hk) * DK, (size_t)HK * DK, p.len, sX, tid);
+  la_tile<DV>(a.z + (p.row0 * a.geo.H + h) * DV, (size_t)a.geo.H * DV, p.len, sZ, tid);
+  la_sums(a.geo, p, h, sG, tid);
+  __syncthreads();
+  if (tid < CH) sW[tid] = REV ? a.geo.scale * la_exp(sG[tid + 1]) : la_exp(sG[CH] - sG[tid + 1]);
+  if (tid == 0) a.eGC[p.ch] = la_exp(sG[CH]);
+  __syncthreads();
+  constexpr int NV = DV / 16;
+  const int g = lane >> 4, l = lane & 15;
+  float* N = a.N + p.ch * (size_t)(DK * DV);
+  for (int cb = wave; cb < DK / 16; cb += kThr / 64) {
+    f4 acc[NV];
+#pragma unroll
+    for (int t = 0; t < NV; ++t) acc[t] = f4{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < CH; s += 4) {
+      const float x = sX[(s + g) * (DK + 4) + 16 * cb + l] * sW[s + g];
+#pragma unroll
+      for (int t = 0; t < NV; ++t) acc[t] = mfma4(x, sZ[(s + g) * (DV + 4) + 16 * t + l], acc[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < NV; ++t)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) N[(16 * cb + 4 * g + u) * DV + 16 * t + l] = acc[t][u];
+  }
+}
+
+// ---- the states that enter the chunks --------------------------------------
+// A thread takes four elements through its sequence; eight chunks' loads are in
+// flight at a time.
+__global__ __launch_bounds__(kThr) void la_combine_kernel(LaCombineArgs a) {
+  constexpr int AHEAD = 8;
+  const int per = a.size / (4 * kThr);
+  const int q = blockIdx.x / per, e = ((blockIdx.x % per) * kThr + threadIdx.x) * 4;
+  const ScanRange rng = scan_range(a.geo.vl, q, a.geo.H, a.geo.T, a.geo.NT);
+  const size_t size = a.size;
+  f4 S = {0.f, 0.f, 0.f, 0.f};
+  if (a.init) S = *reinterpret_cast<const f4*>(a.init + q * size + e);
+  const int n = rng.c1 - rng.c0;
+  for (int i0 = 0; i0 < n; i0 += AHEAD) {
+    f4 x[AHEAD];
+    float d[AHEAD];
+    float* at[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      const int i = min(i0 + j, n - 1);
+      const size_t ch = rng.chs + (a.rev ? rng.c1 - 1 - i : rng.c0 + i);
+      at[j] = a.N + ch * size + e;
+      x[j] = *reinterpret_cast<const f4*>(at[j]);
+      d[j] = a.eGC[ch];
+    }
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      if (i0 + j < n) {
+        *reinterpret_cast<f4*>(at[j]) = S;
+        S = S * d[j] + x[j];
+      }
+    }
+  }
+  if (a.fin) *reinterpret_cast<f4*>(a.fin + q * size + e) = S;
+}
+
+// ---- outputs ---------------------------------------------------------------
+template <int DK, int DV, typename TIn>
+__global__ __launch_bounds__(kThr) void la_fwd_kernel(LaFwdArgs<TIn> a) {
+  __shared__ double sG[CH + 1];
+  extern __shared__ __align__(16) float smem[];
+  float *sQ = smem, *sK = sQ + CH * (DK + 4), *sV = sK + CH * (DK + 4), *sP = sV + CH * (DV + 4);
+  const int tid = threadIdx.x, lane = tid & 63, i = tid >> 6, g = lane >> 4, l = lane & 15;
+  int h;
+  ChunkPos p;
+  if (!la_chunk(a.geo, blockIdx.x, h, p)) return;
+  const int H = a.geo.H, HK = H / a.geo.G, hk = h / a.geo.G;
+  la_tile<DK>(a.q + (p.row0 * HK + hk) * DK, (size_t)HK * DK, p.len, sQ, tid);
+  la_tile<DK>(a.k + (p.row0 * HK + hk) * DK, (size_t)HK * DK, p.len, sK, tid);
+  la_tile<DV>(a.v + (p.row0 * H + h) * DV, (size_t)H * DV, p.len, sV, tid);
+  la_sums(a.geo, p, h, sG, tid);
+  __syncthreads();
+  for (int j = 0; j <= i; ++j) {
+    const f4 x = la_dot_tile<DK>(sQ, sK, 16 * i, 16 * j, lane);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int r = 16 * i + 4 * g + u, s = 16 * j + l;
+      sP[r * LP + s] = s <= r ? x[u] * la_exp(sG[r + 1] - sG[s + 1]) : 0.f;
+    }
+  }
+  __syncthreads();
+  float er[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) er[u] = la_exp(sG[16 * i + 4 * g + u + 1]);
+  const float* S = a.N + p.ch * (size_t)(DK * DV);
+  TIn* o = a.o + (p.row0 * H + h) * DV;
+  for (int t = 0; t < DV / 16; ++t) {
+    f4 acc = la_state_tile<DK, DV>(sQ, S, 16 * i, 16 * t, f4{0.f, 0.f, 0.f, 0.f}, lane);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) acc[u] *= er[u];
+    acc = la_rows_tile<DV>(sP, sV, i, 16 * t, acc, lane);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int r = 16 * i + 4 * g + u;
+      if (r < p.len) la_put(o + (size_t)r * H * DV + 16 * t + l, a.geo.scale * acc[u]);
+    }
+  }
+}
+
+// ---- gradients -------------------------------------------------------------
+template <int DK, int DV, typename TIn>
+__global__ __launch_bounds__(kThr) void la_bwd_kernel(LaBwdArgs<TIn> a) {
+  __shared__ double sG[CH + 1];
+  __shared__ float sA[CH], sB[CH], sRow[CH], sCol[4][CH], sE[kThr / 64];
+  extern __shared__ __align__(16) float smem[];
+  float *sQ = smem, *sK = sQ + CH * (DK + 4), *sV = sK + CH * (DK + 4), *sD = sV + CH * (DV + 4);
+  float* sP = sD + CH * (DV + 4);
+  const int tid = threadIdx.x, lane = tid & 63, i = tid >> 6, g = lane >> 4, l = lane & 15;
+  int h;
+  ChunkPos p;
+  if (!la_chunk(a.geo, blockIdx.x, h, p)) return;
+  const int H = a.geo.H, HK = H / a.geo.G, hk = h / a.geo.G;
+  const float scale = a.geo.scale;
+  la_tile<DK>(a.q + (p.row0 * HK + hk) * DK, (size_t)HK * DK, p.len, sQ, tid);
+  la_tile<DK>(a.k + (p.row0 * HK + hk) * DK, (size_t)HK * DK, p.len, sK, tid);
+  la_tile<DV>(a.v + (p.row0 * H + h) * DV, (size_t)H * DV, p.len, sV, tid);
+  la_tile<DV>(a.dout + (p.row0 * H + h) * DV, (size_t)H * DV, p.len, sD, tid);
+  la_sums(a.geo, p, h, sG, tid);
+  for (int e = tid; e < 4 * CH; e += kThr) sCol[e / CH][e % CH] = 0.f;
+  const float* S = a.N + p.ch * (size_t)(DK * DV);
+  const float* dS = a.M + p.ch * (size_t)(DK * DV);
+  float e0 = 0.f;
+  for (int e = 4 * tid; e < DK * DV; e += 4 * kThr) {
+    const float4 x = ld4(S + e), y = ld4(dS + e);
+    e0 += x.x * y.x + x.y * y.y + x.z * y.z + x.w * y.w;
+  }
+  e0 = row_sum(e0);
+  e0 += row_partner16(e0, (lane & 16) != 0);
+  e0 += row_partner32(e0, lane >= 32);
+  if (lane == 0) sE[i] = e0;
+  __syncthreads();
+
+  // scores of the wave's 16 query rows against every key row up to them
+  f4 wd[4];
+  float rows[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    wd[j] = f4{0.f, 0.f, 0.f, 0.f};
+    if (j > i) continue;
+    f4 x = la_dot_tile<DK>(sQ, sK, 16 * i, 16 * j, lane);
+    const f4 y = la_dot_tile<DV>(sD, sV, 16 * i, 16 * j, lane);
+    float col = 0.f;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int r = 16 * i + 4 * g + u, s = 16 * j + l;
+      const float d = s <= r ? la_exp(sG[r + 1] - sG[s + 1]) : 0.f;
+      const float w = s < r ? scale * d * x[u] * y[u] : 0.f;
+      rows[u] += w;
+      col += w;
+      wd[j][u] = s <= r ? d * y[u] : 0.f;
+      sP[r * LP + s] = s <= r ? d * x[u] : 0.f;
+    }
+    col += row_partner16(col, (lane & 16) != 0);
+    col += row_partner32(col, lane >= 32);
+    if (g == 0) sCol[i][16 * j + l] = col;
+  }
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const float x = row_sum(rows[u]);
+    if (l == 0) sRow[16 * i + 4 * g + u] = x;
+  }
+  __syncthreads();
+
+  float er[4], tail[4];  // of the wave's rows 16 i + 4 g + u
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    er[u] = scale * la_exp(sG[16 * i + 4 * g + u + 1]);
+    tail[u] = la_exp(sG[CH] - sG[16 * i + 4 * g + u + 1]);
+  }
+  // dv, and b_s = v_s . (exp(G_C - G_s) dS^T k_s)
+  float dot[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int t = 0; t < DV / 16; ++t) {
+    f4 inter = la_state_tile<DK, DV>(sK, dS, 16 * i, 16 * t, f4{0.f, 0.f, 0.f, 0.f}, lane);
+    const f4 intra = la_cols_tile<DV>(sP, sD, i, 16 * t, f4{0.f, 0.f, 0.f, 0.f}, lane);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int r = 16 * i + 4 * g + u;
+      inter[u] *= tail[u];
+      dot[u] += inter[u] * sV[r * (DV + 4) + 16 * t + l];
+      if (r < p.len) la_put(a.dv + ((p.row0 + r) * H + h) * DV + 16 * t + l, inter[u] + scale * intra[u]);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const float x = row_sum(dot[u]);
+    if (l == 0) sB[16 * i + 4 * g + u] = x;
+    dot[u] = 0.f;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (j <= i)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) sP[(16 * i + 4 * g + u) * LP + 16 * j + l] = wd[j][u];
+  __syncthreads();
+  // dq, and a_r = q_r . (scale exp(G_r) S0 do_r); dk
+  for (int t = 0; t < DK / 16; ++t) {
+    f4 qi = la_state_t_tile<DV>(sD, S, 16 * i, 16 * t, f4{0.f, 0.f, 0.f, 0.f}, lane);
+    const f4 qa = la_rows_tile<DK>(sP, sK, i, 16 * t, f4{0.f, 0.f, 0.f, 0.f}, lane);
+    const f4 ki = la_state_t_tile<DV>(sV, dS, 16 * i, 16 * t, f4{0.f, 0.f, 0.f, 0.f}, lane);
+    const f4 ka = la_cols_tile<DK>(sP, sQ, i, 16 * t, f4{0.f, 0.f, 0.f, 0.f}, lane);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int r = 16 * i + 4 * g + u;
+      qi[u] *= er[u];
+      dot[u] += qi[u] * sQ[r * (DK + 4) + 16 * t + l];
+      const float dq = qi[u] + scale * qa[u], dk = tail[u] * ki[u] + scale * ka[u];
+      if (r < p.len) {
+        if (a.Pq) {
+          const size_t at = ((p.row0 + r) * H + h) * DK + 16 * t + l;
+          a.Pq[at] = dq;
+          a.Pk[at] = dk;
+        } else {
+          const size_t at = ((p.row0 + r) * HK + hk) * DK + 16 * t + l;
+          la_put(a.dq + at, dq);
+          la_put(a.dk + at, dk);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const float x = row_sum(dot[u]);
+    if (l == 0) sA[16 * i + 4 * g + u] = x;
+  }
+  __syncthreads();
+  if (tid < 64) {
+    // E + sum_{r>=t} a_r + sum_{s<t} (b_s + col_s - row_s)
+    double x = (double)sB[tid] + (((double)sCol[0][tid] + sCol[1][tid]) + ((double)sCol[2][tid] + sCol[3][tid])) - sRow[tid];
+    double y = sA[tid];
+    const double own_x = x;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const double px = __shfl_up(x, o), py = __shfl_down(y, o);
+      if (tid >= o) x += px;
+      if (tid + o < 64) y += py;
+    }
+    const double E = (double)la_exp(sG[CH]) * (((double)sE[0] + sE[1]) + ((double)sE[2] + sE[3]));
+    if (tid < p.len) a.dg[(p.row0 + tid) * H + h] = (float)(E + y + (x - own_x));
+  }
+}
+
+// ---- sums over a group's value heads, and over the tokens ------------------
+template <typename TOut>
+__global__ __launch_bounds__(256) void la_group_kernel(const float* P, TOut* out, size_t n4, int G, int D) {
+  const size_t stride = (size_t)gridDim.x * blockDim.x;
+  for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < n4; i += stride) {
+    const size_t c = 4 * i % D, rh = 4 * i / D;
+    const float* src = P + rh * G * D + c;
+    f4 acc = *reinterpret_cast<const f4*>(src);
+    for (int j = 1; j < G; ++j) acc += *reinterpret_cast<const f4*>(src + (size_t)j * D);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) la_put(out + 4 * i + u, acc[u]);
+  }
+}
+
+__global__ __launch_bounds__(1024) void la_headsum_kernel(const float* P, float* dg, size_t rows, int H) {
+  __shared__ double sum[1024];
+  const int tid = threadIdx.x, h = blockIdx.x;
+  double x = 0.0;
+  for (size_t r = tid; r < rows; r += 1024) x += P[r * H + h];
+  sum[tid] = x;
+  __syncthreads();
+  for (int o = 512; o > 0; o >>= 1) {
+    if (tid < o) sum[tid] += sum[tid + o];
+    __syncthreads();
+  }
+  if (tid == 0) dg[h] = (float)sum[0];
+}
+
+// ---- launches --------------------------------------------------------------
+namespace {
+unsigned la_units(const LaGeo& g) { return (unsigned)g.NT * g.H * g.B; }
+template <class K>
+hipError_t la_lds(K kernel, size_t bytes) {
+  return hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+}  // namespace
+
+template <int DK, int DV, typename TIn>
+hipError_t launch_la_state(const LaStateArgs<TIn>& a, bool rev, hipStream_t st) {
+  constexpr size_t lds = 4 * CH * (DK + DV + 8);
+  const auto kernel = rev ? la_state_kernel<DK, DV, TIn, true> : la_state_kernel<DK, DV, TIn, false>;
+  hipError_t e = la_lds(kernel, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3(la_units(a.geo)), dim3(kThr), lds, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_la_combine(const LaCombineArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL(la_combine_kernel, dim3((unsigned)(a.nseq * a.geo.H * (a.size / (4 * kThr)))), dim3(kThr), 0, st, a);
+  return hipGetLastError();
+}
+
+template <int DK, int DV, typename TIn>
+hipError_t launch_la_fwd(const LaFwdArgs<TIn>& a, hipStream_t st) {
+  constexpr size_t lds = 4 * CH * (2 * (DK + 4) + DV + 4 + LP);
+  hipError_t e = la_lds(la_fwd_kernel<DK, DV, TIn>, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((la_fwd_kernel<DK, DV, TIn>), dim3(la_units(a.geo)), dim3(kThr), lds, st, a);
+  return hipGetLastError();
+}
+
+template <int DK, int DV, typename TIn>
+hipError_t launch_la_bwd(const LaBwdArgs<TIn>& a, hipStream_t st) {
+  constexpr size_t lds = 4 * CH * (2 * (DK + 4) + 2 * (DV + 4) + LP);
+  hipError_t e = la_lds(la_bwd_kernel<DK, DV, TIn>, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((la_bwd_kernel<DK, DV, TIn>), dim3(la_units(a.geo)), dim3(kThr), lds, st, a);
+  return hipGetLastError();
+}
+
+template <typename TOut>
+hipError_t launch_la_group(const float* P, TOut* out, size_t rows, int Hk, int G, int D, hipStream_t st) {
+  const size_t n4 = rows * Hk * (size_t)D / 4, blocks = (n4 + 255) / 256;
+  hipLaunchKernelGGL(la_group_kernel<TOut>, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), 0, st, P, out,
+                     n4, G, D);
+  return hipGetLastError();
+}
+template hipError_t launch_la_group<float>(const float*, float*, size_t, int, int, int, hipStream_t);
+template hipError_t launch_la_group<bf16_t>(const float*, bf16_t*, size_t, int, int, int, hipStream_t);
+
+hipError_t launch_la_headsum(const float* P, float* dg, size_t rows, int H, hipStream_t st) {
+  hipLaunchKernelGGL(la_headsum_kernel, dim3((unsigned)H), dim3(1024), 0, st, P, dg, rows, H);
+  return hipGetLastError();
+}
+
+#define GDR2_LA_INST(DK, DV, T)                                                                   \
+  template hipError_t launch_la_state<DK, DV, T>(const LaStateArgs<T>&, bool, hipStream_t);       \
+  template hipError_t launch_la_fwd<DK, DV, T>(const LaFwdArgs<T>&, hipStream_t);                 \
+  template hipError_t launch_la_bwd<DK, DV, T>(const LaBwdArgs<T>&, hipStream_t);
+#define GDR2_LA_INST4(T) \
+  GDR2_LA_INST(64, 64, T) GDR2_LA_INST(64, 128, T) GDR2_LA_INST(128, 64, T) GDR2_LA_INST(128, 128, T)
+GDR2_LA_INST4(float)
+GDR2_LA_INST4(bf16_t)
+
+}  // namespace gdr2
