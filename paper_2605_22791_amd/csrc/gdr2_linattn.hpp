@@ -77,6 +77,45 @@ struct LaCombineArgs {
   int nseq, size, rev;      // sequences, Dk * Dv
 };
 
+// ---- bf16 problems: scans over segments ------------------------------------
+// A sequence is cut into segments of seg_tokens tokens (a multiple of 64; an empty
+// sequence has one without tokens); slot = sequence * nseg + segment, or, packed, an
+// entry of a table: first token, tokens and sequence of every slot, and the first
+// slot of every sequence.
+struct LaSegs {
+  const int *t0 = nullptr, *len = nullptr, *seq = nullptr, *off = nullptr;  // packed only
+  int nseq, nseg, nslot, seg_tokens;
+};
+
+// Chunks between two of the points where the decay gradient's running sum starts anew
+// from <S, dS> (LaScanArgs).
+constexpr int kLaAnchor = 16;
+
+struct LaScanArgs {
+  LaGeo geo;
+  LaSegs segs;
+  const bf16_t *q, *k, *v, *dout;
+  const float *S0, *dST;  // nullable
+  float *S, *dS, *dec;    // states behind the segments (gradients before them), exp(sum g): (slot, H)
+  bf16_t* o;
+  float *ST, *dS0;  // nullable
+  bf16_t *dq, *dk, *dv;
+  float *Pq, *Pk;        // grouped heads: dq, dk of each value head
+  float *pa, *pb, *prc;  // a_r, b_s by column slice (slice, row, H); row sums less column sums of W (row, H)
+  float *aS, *aD;        // S and dS at the anchors, (slot, H, anchors a segment)
+  float* dg;             // (rows, H)
+  int anchors;
+};
+
+template <int DK, int DV>
+hipError_t launch_la_segstate(const LaScanArgs& a, bool rev, hipStream_t st);
+hipError_t launch_la_segcombine(const LaScanArgs& a, int size, bool rev, hipStream_t st);
+template <int DK, int DV>
+hipError_t launch_la_scan_fwd(const LaScanArgs& a, hipStream_t st);
+template <int DK, int DV>
+hipError_t launch_la_scan_bwd(const LaScanArgs& a, hipStream_t st);
+hipError_t launch_la_segtable(const int* cu, const LaSegs& s, int T, int* t0, int* len, int* seq, int* off, hipStream_t st);
+
 template <typename TIn>
 struct LaStepArgs {
   const TIn *q, *k, *v;

@@ -13,51 +13,97 @@ namespace {
 
 bool decay_ok(int d) { return d == GDR2_DECAY_TOKEN || d == GDR2_DECAY_HEAD; }
 
-// Workspace: chunk states N (and the gradients M of the chunks' end states), exp(G_C),
-// the chunk table of a packed call and, backward, the per-value-head parts of grouped
-// heads and the per-token decay gradients of per-head decays.
+// fp32 problems: chunk states N (and the gradients M of the chunks' end states), exp(G_C)
+// and the chunk table of a packed call.  bf16 problems: the states behind the segments (the
+// gradients before them), the segments' decays, the segment table of a packed call and,
+// backward, the terms of the decays' gradient with S and dS at its anchors.  Both, backward:
+// the per-value-head parts of grouped heads, the per-token gradients of per-head decays.
 struct LaLayout {
   size_t N, M, eGC, coff, ct0, clen, sord, Pq, Pk, dg, total;
+  size_t S, dS, dec, st0, slen, sseq, soff, pa, pb, prc, aS, aD;
   int NT;
+  LaSegs segs;
+  int anchors;
+  bool multi;  // sequences of more than one segment
 };
+
+// Tokens of a segment.  A workgroup scans 64 columns of one head's segment; whole sequences
+// while there are enough of those to give every CU one, else cut until there are, down to two
+// chunks.  A packed batch counts as one sequence: its lengths are on the device.
+int la_seg_tokens(const gdr2_problem* p, int nseq) {
+  const int NT = chunks_per_seq(p);
+  const long long base = (long long)(nseq > 0 ? 1 : p->B) * value_view(p).H * (p->Dv / 64);
+  int chunks = NT;
+  while (base * ((NT + chunks - 1) / chunks) < 256 && chunks > 2) chunks = (chunks + 1) / 2;
+  return chunks * CH;
+}
 
 LaLayout la_layout(const gdr2_problem* p, bool bwd, int nseq) {
   const gdr2_problem v = value_view(p);
   const int G = group_of(p);
+  const size_t state = (size_t)p->Dk * p->Dv, rows = (size_t)p->B * p->T;
   LaLayout L{};
-  L.NT = nseq > 0 ? varlen_slots(p, nseq) : chunks_per_seq(p);
-  const size_t NC = (size_t)v.H * L.NT * (nseq > 0 ? 1 : p->B), state = (size_t)p->Dk * p->Dv;
   size_t off = 0;
   const auto take = [&](size_t words) {
     const size_t at = off;
     off += round_up(4 * words);
     return at;
   };
-  L.N = take(NC * state);
-  L.eGC = take(NC);
-  if (nseq > 0) {
-    L.coff = take((size_t)nseq + 1);
-    L.ct0 = take(L.NT);
-    L.clen = take(L.NT);
-    L.sord = take(nseq);
+  if (p->dtype == GDR2_BF16) {
+    LaSegs& s = L.segs;
+    s.seg_tokens = la_seg_tokens(p, nseq);
+    s.nseq = nseq > 0 ? nseq : p->B;
+    s.nseg = (p->T + s.seg_tokens - 1) / s.seg_tokens;
+    s.nslot = nseq > 0 ? p->T / s.seg_tokens + nseq : p->B * s.nseg;
+    L.anchors = (s.seg_tokens / CH + kLaAnchor - 1) / kLaAnchor;
+    L.multi = s.nseg > 1;
+    const size_t units = (size_t)s.nslot * v.H;
+    if (nseq > 0) {
+      L.st0 = take(s.nslot);
+      L.slen = take(s.nslot);
+      L.sseq = take(s.nslot);
+      L.soff = take((size_t)nseq + 1);
+    }
+    if (L.multi) {
+      L.S = take(units * state);
+      L.dec = take(units);
+    }
+    if (bwd) {
+      if (L.multi) L.dS = take(units * state);
+      L.aS = take(units * L.anchors * state);
+      L.aD = take(units * L.anchors * state);
+      L.pa = take(rows * v.H * (p->Dk / 64));
+      L.pb = take(rows * v.H * ((p->Dk > p->Dv ? p->Dk : p->Dv) / 64));
+      L.prc = take(rows * v.H);
+    }
+  } else {
+    L.NT = nseq > 0 ? varlen_slots(p, nseq) : chunks_per_seq(p);
+    const size_t NC = (size_t)v.H * L.NT * (nseq > 0 ? 1 : p->B);
+    L.N = take(NC * state);
+    L.eGC = take(NC);
+    if (nseq > 0) {
+      L.coff = take((size_t)nseq + 1);
+      L.ct0 = take(L.NT);
+      L.clen = take(L.NT);
+      L.sord = take(nseq);
+    }
+    if (bwd) L.M = take(NC * state);
   }
   if (bwd) {
-    const size_t rows = (size_t)p->B * p->T;
-    L.M = take(NC * state);
     if (G > 1) {
       L.Pq = take(rows * v.H * p->Dk);
       L.Pk = take(rows * v.H * p->Dk);
     }
     L.dg = take(rows * v.H);
   }
-  L.total = off;
+  L.total = off > 0 ? off : kAlign;  // a call always takes a workspace
   return L;
 }
 
 LaGeo la_geo(const gdr2_problem* p, const LaLayout& L, int decay, const int32_t* cu, int nseq, const float* g, void* ws) {
   LaGeo a{};
   const gdr2_problem v = value_view(p);
-  if (nseq > 0) {
+  if (nseq > 0 && p->dtype == GDR2_FP32) {
     a.vl.cu = cu;
     a.vl.coff = at<int>(ws, L.coff);
     a.vl.ct0 = at<int>(ws, L.ct0);
@@ -79,6 +125,9 @@ LaGeo la_geo(const gdr2_problem* p, const LaLayout& L, int decay, const int32_t*
 
 hipError_t la_table(const gdr2_problem* p, const LaLayout& L, const int32_t* cu, int nseq, void* ws, hipStream_t st) {
   if (nseq == 0) return hipSuccess;
+  if (p->dtype == GDR2_BF16)
+    return launch_la_segtable(cu, L.segs, p->T, at<int>(ws, L.st0), at<int>(ws, L.slen), at<int>(ws, L.sseq),
+                              at<int>(ws, L.soff), st);
   return launch_varlen_table(cu, nseq, p->T, L.NT, at<int>(ws, L.coff), at<int>(ws, L.ct0), at<int>(ws, L.clen),
                              at<int>(ws, L.sord), st);
 }
@@ -93,14 +142,51 @@ hipError_t la_states(const LaGeo& geo, int ns, const void* x, const void* z, flo
   return launch_la_combine({geo, N, eGC, init, fin, ns, DK * DV, rev ? 1 : 0}, st);
 }
 
+LaScanArgs la_scan_args(const LaLayout& L, const LaGeo& geo, int nseq, const void* q, const void* k, const void* v,
+                        const float* S0, void* ws) {
+  LaScanArgs a{};
+  a.geo = geo;
+  a.segs = L.segs;
+  if (nseq > 0) {
+    a.segs.t0 = at<int>(ws, L.st0);
+    a.segs.len = at<int>(ws, L.slen);
+    a.segs.seq = at<int>(ws, L.sseq);
+    a.segs.off = at<int>(ws, L.soff);
+  }
+  a.q = static_cast<const bf16_t*>(q);
+  a.k = static_cast<const bf16_t*>(k);
+  a.v = static_cast<const bf16_t*>(v);
+  a.S0 = S0;
+  a.S = at<float>(ws, L.S);
+  a.dS = at<float>(ws, L.dS);
+  a.dec = at<float>(ws, L.dec);
+  a.anchors = L.anchors;
+  return a;
+}
+
+// the states behind the segments (rev: the gradients before them)
+template <int DK, int DV>
+hipError_t la_seg_states(const LaScanArgs& a, bool rev, hipStream_t st) {
+  const hipError_t e = launch_la_segstate<DK, DV>(a, rev, st);
+  return e != hipSuccess ? e : launch_la_segcombine(a, DK * DV, rev, st);
+}
+
 template <int DK, int DV, typename TIn>
-hipError_t la_fwd(const gdr2_problem* p, const LaLayout& L, const LaGeo& geo, int ns, const void* q, const void* k,
+hipError_t la_fwd(const gdr2_problem* p, const LaLayout& L, const LaGeo& geo, int nseq, const void* q, const void* k,
                   const void* v, const float* S0, void* o, float* ST, void* ws, hipStream_t st) {
-  float *N = at<float>(ws, L.N), *eGC = at<float>(ws, L.eGC);
-  hipError_t e = la_states<DK, DV, TIn>(geo, ns, k, v, N, eGC, S0, ST, false, st);
-  if (e != hipSuccess) return e;
-  return launch_la_fwd<DK, DV, TIn>({geo, static_cast<const TIn*>(q), static_cast<const TIn*>(k),
-                                     static_cast<const TIn*>(v), static_cast<TIn*>(o), S0, N, eGC}, st);
+  if constexpr (std::is_same<TIn, bf16_t>::value) {
+    LaScanArgs a = la_scan_args(L, geo, nseq, q, k, v, S0, ws);
+    a.o = static_cast<bf16_t*>(o);
+    a.ST = ST;
+    hipError_t e = L.multi ? la_seg_states<DK, DV>(a, false, st) : hipSuccess;
+    return e != hipSuccess ? e : launch_la_scan_fwd<DK, DV>(a, st);
+  } else {
+    float *N = at<float>(ws, L.N), *eGC = at<float>(ws, L.eGC);
+    hipError_t e = la_states<DK, DV, TIn>(geo, nseq > 0 ? nseq : p->B, k, v, N, eGC, S0, ST, false, st);
+    if (e != hipSuccess) return e;
+    return launch_la_fwd<DK, DV, TIn>({geo, static_cast<const TIn*>(q), static_cast<const TIn*>(k),
+                                       static_cast<const TIn*>(v), static_cast<TIn*>(o), S0, N, eGC}, st);
+  }
 }
 
 struct LaGrads {
@@ -109,36 +195,45 @@ struct LaGrads {
 };
 
 template <int DK, int DV, typename TIn>
-hipError_t la_bwd(const gdr2_problem* p, const LaLayout& L, const LaGeo& geo, int ns, const void* q, const void* k,
+hipError_t la_bwd(const gdr2_problem* p, const LaLayout& L, const LaGeo& geo, int nseq, const void* q, const void* k,
                   const void* v, const float* S0, const void* dout, const float* dST, const LaGrads& d, void* ws,
                   bool saved, hipStream_t st) {
-  float *N = at<float>(ws, L.N), *M = at<float>(ws, L.M), *eGC = at<float>(ws, L.eGC);
-  hipError_t e = hipSuccess;
-  if (!saved) e = la_states<DK, DV, TIn>(geo, ns, k, v, N, eGC, S0, nullptr, false, st);
-  if (e == hipSuccess) e = la_states<DK, DV, TIn>(geo, ns, q, dout, M, eGC, dST, d.dS0, true, st);
-  if (e != hipSuccess) return e;
   const size_t rows = (size_t)p->B * p->T;
-  LaBwdArgs<TIn> a{};
-  a.geo = geo;
-  a.q = static_cast<const TIn*>(q);
-  a.k = static_cast<const TIn*>(k);
-  a.v = static_cast<const TIn*>(v);
-  a.dout = static_cast<const TIn*>(dout);
-  a.dq = static_cast<TIn*>(d.dq);
-  a.dk = static_cast<TIn*>(d.dk);
-  a.dv = static_cast<TIn*>(d.dv);
-  if (geo.G > 1) {
-    a.Pq = at<float>(ws, L.Pq);
-    a.Pk = at<float>(ws, L.Pk);
+  float *Pq = geo.G > 1 ? at<float>(ws, L.Pq) : nullptr, *Pk = geo.G > 1 ? at<float>(ws, L.Pk) : nullptr;
+  float* dg = geo.per_head ? at<float>(ws, L.dg) : d.dg;
+  hipError_t e = hipSuccess;
+  if constexpr (std::is_same<TIn, bf16_t>::value) {
+    LaScanArgs a = la_scan_args(L, geo, nseq, q, k, v, S0, ws);
+    a.dout = static_cast<const bf16_t*>(dout);
+    a.dST = dST;
+    a.dS0 = d.dS0;
+    a.dq = static_cast<bf16_t*>(d.dq);
+    a.dk = static_cast<bf16_t*>(d.dk);
+    a.dv = static_cast<bf16_t*>(d.dv);
+    a.Pq = Pq;
+    a.Pk = Pk;
+    a.pa = at<float>(ws, L.pa);
+    a.pb = at<float>(ws, L.pb);
+    a.prc = at<float>(ws, L.prc);
+    a.aS = at<float>(ws, L.aS);
+    a.aD = at<float>(ws, L.aD);
+    a.dg = dg;
+    if (L.multi && !saved) e = la_seg_states<DK, DV>(a, false, st);
+    if (L.multi && e == hipSuccess) e = la_seg_states<DK, DV>(a, true, st);
+    if (e == hipSuccess) e = launch_la_scan_bwd<DK, DV>(a, st);
+  } else {
+    const int ns = nseq > 0 ? nseq : p->B;
+    float *N = at<float>(ws, L.N), *M = at<float>(ws, L.M), *eGC = at<float>(ws, L.eGC);
+    if (!saved) e = la_states<DK, DV, TIn>(geo, ns, k, v, N, eGC, S0, nullptr, false, st);
+    if (e == hipSuccess) e = la_states<DK, DV, TIn>(geo, ns, q, dout, M, eGC, dST, d.dS0, true, st);
+    if (e != hipSuccess) return e;
+    e = launch_la_bwd<DK, DV, TIn>({geo, static_cast<const TIn*>(q), static_cast<const TIn*>(k),
+                                    static_cast<const TIn*>(v), static_cast<const TIn*>(dout), static_cast<TIn*>(d.dq),
+                                    static_cast<TIn*>(d.dk), static_cast<TIn*>(d.dv), Pq, Pk, dg, N, M, eGC}, st);
   }
-  a.dg = geo.per_head ? at<float>(ws, L.dg) : d.dg;
-  a.N = N;
-  a.M = M;
-  a.eGC = eGC;
-  e = launch_la_bwd<DK, DV, TIn>(a, st);
-  if (e == hipSuccess && geo.G > 1) e = launch_la_group<TIn>(a.Pq, a.dq, rows, geo.H / geo.G, geo.G, DK, st);
-  if (e == hipSuccess && geo.G > 1) e = launch_la_group<TIn>(a.Pk, a.dk, rows, geo.H / geo.G, geo.G, DK, st);
-  if (e == hipSuccess && geo.per_head) e = launch_la_headsum(a.dg, d.dg, rows, geo.H, st);
+  if (e == hipSuccess && geo.G > 1) e = launch_la_group<TIn>(Pq, static_cast<TIn*>(d.dq), rows, geo.H / geo.G, geo.G, DK, st);
+  if (e == hipSuccess && geo.G > 1) e = launch_la_group<TIn>(Pk, static_cast<TIn*>(d.dk), rows, geo.H / geo.G, geo.G, DK, st);
+  if (e == hipSuccess && geo.per_head) e = launch_la_headsum(dg, d.dg, rows, geo.H, st);
   return e;
 }
 
@@ -189,11 +284,10 @@ gdr2_status gdr2_linattn_fwd(const gdr2_problem* p, int32_t decay, const int32_t
   const LaLayout L = la_layout(p, save != 0, n_seqs);
   if (ws_bytes < L.total) return GDR2_EWORKSPACE;
   const LaGeo geo = la_geo(p, L, decay, cu, n_seqs, g, ws);
-  const int ns = n_seqs > 0 ? n_seqs : p->B;
   hipError_t e = la_table(p, L, cu, n_seqs, ws, stream);
   if (e == hipSuccess)
     e = la_dispatch(p, [&](auto dk, auto dv, auto t) {
-      return la_fwd<decltype(dk)::value, decltype(dv)::value, decltype(t)>(p, L, geo, ns, q, k, v, S0, o, S_T, ws, stream);
+      return la_fwd<decltype(dk)::value, decltype(dv)::value, decltype(t)>(p, L, geo, n_seqs, q, k, v, S0, o, S_T, ws, stream);
     });
   return hip_status(e, stream);
 }
@@ -210,12 +304,11 @@ gdr2_status gdr2_linattn_bwd(const gdr2_problem* p, int32_t decay, const int32_t
   const LaLayout L = la_layout(p, true, n_seqs);
   if (ws_bytes < L.total) return GDR2_EWORKSPACE;
   const LaGeo geo = la_geo(p, L, decay, cu, n_seqs, g, ws);
-  const int ns = n_seqs > 0 ? n_seqs : p->B;
   const LaGrads d{dq, dk, dv, dg, dS0};
   hipError_t e = saved ? hipSuccess : la_table(p, L, cu, n_seqs, ws, stream);
   if (e == hipSuccess)
     e = la_dispatch(p, [&](auto ck, auto cv, auto t) {
-      return la_bwd<decltype(ck)::value, decltype(cv)::value, decltype(t)>(p, L, geo, ns, q, k, v, S0, dout, dS_T, d, ws,
+      return la_bwd<decltype(ck)::value, decltype(cv)::value, decltype(t)>(p, L, geo, n_seqs, q, k, v, S0, dout, dS_T, d, ws,
                                                                            saved != 0, stream);
     });
   return hip_status(e, stream);

@@ -492,6 +492,5 @@ hipError_t launch_la_headsum(const float* P, float* dg, size_t rows, int H, hipS
 #define GDR2_LA_INST4(T) \
   GDR2_LA_INST(64, 64, T) GDR2_LA_INST(64, 128, T) GDR2_LA_INST(128, 64, T) GDR2_LA_INST(128, 128, T)
 GDR2_LA_INST4(float)
-GDR2_LA_INST4(bf16_t)
 
 }  // namespace gdr2
