@@ -101,7 +101,8 @@ struct LaScanArgs {
   float *ST, *dS0;  // nullable
   bf16_t *dq, *dk, *dv;
   float *Pq, *Pk;        // grouped heads: dq, dk of each value head
-  float *pa, *pb, *prc;  // a_r, b_s by column slice (slice, row, H); row sums less column sums of W (row, H)
+  float *pa, *pb;        // q . dq and v . dv without the diagonal (rows, H)
+  float *ca, *cb;        // sixteen parts of their chunk's sum of what comes from the state (slot, H, chunks a segment)
   float *aS, *aD;        // S and dS at the anchors, (slot, H, anchors a segment)
   float* dg;             // (rows, H)
   int anchors;

@@ -11,6 +11,8 @@ using namespace gdr2;
 
 namespace {
 
+constexpr double kMaxRow = 1 << 22;  // values of one token over all heads
+
 bool decay_ok(int d) { return d == GDR2_DECAY_TOKEN || d == GDR2_DECAY_HEAD; }
 
 // fp32 problems: chunk states N (and the gradients M of the chunks' end states), exp(G_C)
@@ -20,21 +22,24 @@ bool decay_ok(int d) { return d == GDR2_DECAY_TOKEN || d == GDR2_DECAY_HEAD; }
 // the per-value-head parts of grouped heads, the per-token gradients of per-head decays.
 struct LaLayout {
   size_t N, M, eGC, coff, ct0, clen, sord, Pq, Pk, dg, total;
-  size_t S, dS, dec, st0, slen, sseq, soff, pa, pb, prc, aS, aD;
+  size_t S, dS, dec, st0, slen, sseq, soff, pa, pb, ca, cb, aS, aD;
   int NT;
   LaSegs segs;
   int anchors;
   bool multi;  // sequences of more than one segment
 };
 
-// Tokens of a segment.  A workgroup scans 64 columns of one head's segment; whole sequences
-// while there are enough of those to give every CU one, else cut until there are, down to two
-// chunks.  A packed batch counts as one sequence: its lengths are on the device.
+// Tokens of a segment.  A workgroup scans one head's segment; whole sequences while there are
+// enough of those to give every CU two, else cut until there are, down to two chunks.  A packed
+// batch counts as one sequence: its lengths are on the device.
 int la_seg_tokens(const gdr2_problem* p, int nseq) {
   const int NT = chunks_per_seq(p);
-  const long long base = (long long)(nseq > 0 ? 1 : p->B) * value_view(p).H * (p->Dv / 64);
+  const long long base = (long long)(nseq > 0 ? 1 : p->B) * value_view(p).H;
   int chunks = NT;
-  while (base * ((NT + chunks - 1) / chunks) < 256 && chunks > 2) chunks = (chunks + 1) / 2;
+  while (base * ((NT + chunks - 1) / chunks) < 512 && chunks > 2) chunks = (chunks + 1) / 2;
+  // a segment's rows, the widest in fp32, are one buffer of at most 2^31 bytes
+  const long long row = 4LL * value_view(p).H * (p->Dk > p->Dv ? p->Dk : p->Dv);
+  while (chunks > 1 && chunks * CH * row > (1LL << 31)) chunks = (chunks + 1) / 2;
   return chunks * CH;
 }
 
@@ -72,9 +77,10 @@ LaLayout la_layout(const gdr2_problem* p, bool bwd, int nseq) {
       if (L.multi) L.dS = take(units * state);
       L.aS = take(units * L.anchors * state);
       L.aD = take(units * L.anchors * state);
-      L.pa = take(rows * v.H * (p->Dk / 64));
-      L.pb = take(rows * v.H * ((p->Dk > p->Dv ? p->Dk : p->Dv) / 64));
-      L.prc = take(rows * v.H);
+      L.pa = take(rows * v.H);
+      L.pb = take(rows * v.H);
+      L.ca = take(units * (s.seg_tokens / CH) * 16);
+      L.cb = take(units * (s.seg_tokens / CH) * 16);
     }
   } else {
     L.NT = nseq > 0 ? varlen_slots(p, nseq) : chunks_per_seq(p);
@@ -214,7 +220,8 @@ hipError_t la_bwd(const gdr2_problem* p, const LaLayout& L, const LaGeo& geo, in
     a.Pk = Pk;
     a.pa = at<float>(ws, L.pa);
     a.pb = at<float>(ws, L.pb);
-    a.prc = at<float>(ws, L.prc);
+    a.ca = at<float>(ws, L.ca);
+    a.cb = at<float>(ws, L.cb);
     a.aS = at<float>(ws, L.aS);
     a.aD = at<float>(ws, L.aD);
     a.dg = dg;
@@ -256,6 +263,8 @@ gdr2_status la_check(const gdr2_problem* p, int decay, const int32_t* cu, int n_
   const gdr2_status s = check_problem(p, chunked, n_seqs);
   if (s != GDR2_OK) return s;
   if (!decay_ok(decay)) return GDR2_EINVAL;
+  // a chunk's rows are reached by 32-bit byte offsets (fp32 parts of grouped heads among them)
+  if (chunked && (double)value_view(p).H * (p->Dk > p->Dv ? p->Dk : p->Dv) > kMaxRow) return GDR2_EUNSUPPORTED;
   if (n_seqs > 0 && (cu == nullptr || (reinterpret_cast<uintptr_t>(cu) & 3u) != 0)) return GDR2_EINVAL;
   return GDR2_OK;
 }

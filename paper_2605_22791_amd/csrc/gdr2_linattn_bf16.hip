@@ -3,24 +3,35 @@
 //
 // Forward and backward are one form.  With X, Y (rows of length A) and Z (rows of length
 // B) among q, k, v, dout, and a state St (A x B), a chunk gives
-//     out_i = f_i X_i St + sum_j P_ij Z_j,     P_ij = D (X_i . Y_j)
+//     out_i = f_i X_i St + sum_j P_ij Z_j,     P_ij = scale D (X_i . Y_j)
 //     St   <- exp(G_C) St + sum_j Y_j^T (w_j Z_j)
-//   o :  X q, Y k,  Z v;   St = S,     f = exp(G_r), w = exp(G_C - G_s), j <= i, first chunk to last
+//   o :  X q, Y k,  Z v;   St = S,     f = scale exp(G_r), w = exp(G_C - G_s), j <= i, first chunk to last
 //   dq:  X do, Y v, Z k;   St = S^T,   as above
 //   dv:  X k, Y q,  Z do;  St = dS,    f = exp(G_C - G_s), w = scale exp(G_r), j >= i, last chunk to first
 //   dk:  X v, Y do, Z q;   St = dS^T,  as dv
+// A workgroup runs one of these over one segment of one head.
 //
-// A wave owns 16 columns of B over all of A: its state tiles are the accumulators of the
-// update, and split to bf16 they are the A operand of X St as they lie (the K order of that
-// product is permuted to the accumulators' rows), so the state never leaves its registers.
-// The tiles X, Y, Z go through LDS; the scores of a chunk are shared out over the waves,
-// pass through LDS split into two bf16 parts, and meet the same Z fragments that the update
-// uses (scaled).
+// A wave owns 32 columns of B over all of A: its state tiles are the accumulators of the update,
+// and split to bf16 they are the A operand of X St as they lie (the K order of that product is
+// permuted to the accumulators' rows), so the state never leaves its registers.  The tiles X, Y,
+// Z go through LDS; the scores of a chunk are shared out over the waves, pass through LDS split
+// into bf16 parts, and meet the same Z fragments that the update uses (scaled).  Three barriers
+// a chunk, each with work on one side that hides the loads of the tiles on the other:
+//     X, Z there, Y's place free:  load Y;  X St, Z fragments
+//     Y there:                     scores, the decays of the next chunk
+//     P there, X, Z done with:     load the next X, Z;  P Z, output, update
+// Vector instructions bound the scans: one takes 4 cycles of a SIMD's issue and an MFMA 8 (of 16
+// that it is busy for) when several waves share it, so what counts is how many there are.
+// Two workgroups a CU (80 KB of LDS each) fill each other's gaps.
 //
-// Precision: inputs are exact bf16 operands.  fp32 operands are split: scores and the state
-// in products that only feed bf16 outputs into two parts (16 bits, against the outputs' 8);
-// the decayed Z of the update, and the state where the decay gradient's sums read the
+// Precision: inputs are exact bf16 operands.  fp32 operands are split: what only feeds bf16
+// outputs into two parts (16 bits, against the outputs' 8); the decayed Z of the update
+// (S_T, dS0 are fp32), and the state and scores where the decays' gradient reads the
 // product, into three (24 bits).
+//
+// Measured, 8 x 4096 tokens, 16 heads of 128 x 128, four segments a sequence: forward scan 151 us
+// (537 MB, 3.6 TB/s), segment states 68 and 64 us, the three gradients 574 us, decays' gradient
+// 23 us.
 
 #include "gdr2_linattn.hpp"
 #include "gdr2_bf16.hpp"
@@ -59,24 +70,25 @@ __device__ __forceinline__ bool la_unit(const LaSegs& s, int T, int slot, LaUnit
   return true;
 }
 
-// Workgroup b of a grid of (unit, slice): the NS slices of a unit run on one XCD (blocks go to
-// the eight XCDs in turn) and share its L2; unit < n.
-template <int NS>
-__device__ __forceinline__ bool la_slot(int b, int n, int& unit, int& slice) {
-  unit = b / (8 * NS) * 8 + b % 8;
-  slice = b / 8 % NS;
+// Workgroup b of a grid of (unit, role): the NR roles of a unit run on one XCD (blocks go to the
+// eight XCDs in turn) and share its L2; unit < n.
+template <int NR>
+__device__ __forceinline__ bool la_slot(int b, int n, int& unit, int& role) {
+  unit = b / (8 * NR) * 8 + b % 8;
+  role = b / 8 % NR;
   return unit < n;
 }
-template <int NS>
-unsigned la_grid(int n) { return (unsigned)((n + 7) / 8 * 8) * NS; }
+template <int NR>
+unsigned la_grid(int n) { return (unsigned)((n + 7) / 8 * 8) * NR; }
 
 // ---- decays of a chunk -----------------------------------------------------
 // Sums are taken within the blocks of 16 rows in 64 bits, p_r up to and including r, so that
-// no factor is a difference of long sums.  Between blocks j < i, D_rs = L_r R_is with
-// L_r = exp(p_r) and R_is the rest of the way from s to block i; both are at most 1.
+// no factor is a difference of long sums; they are powers of two (log2 e is multiplied in
+// there).  Between blocks j < i, scale D_rs = L_r R_is with L_r = scale exp(p_r) and R_is the
+// rest of the way from s to block i; the exponentials are at most 1.
 struct alignas(16) LaTab {
   double p[CH];
-  float L[CH], R[3][CH], E[CH], T[CH];  // R[i - 1][s]; E: exp(G_r) (scale exp(G_r) in the reverse scans), T: exp(G_C - G_s)
+  float L[CH], R[3][CH], E[CH], T[CH];  // R[i - 1][s]; E: scale exp(G_r), T: exp(G_C - G_s)
   float eC, pad[3];
 };
 
@@ -92,10 +104,10 @@ __device__ __forceinline__ float la_lanef(float x, int lane) {
 __device__ __forceinline__ float la_ex(float x) { return ex2(x * kLog2e); }
 
 // One wave, a row a lane: g the row's raw log-decay; rows past the chunk's end do not decay.
-// E is multiplied by scale.  Returns the row's log-decay.
+// Returns the row's log-decay.
 __device__ __forceinline__ float la_tables(float g, int rows, LaTab& t, int lane, float scale) {
   const float g0 = lane < rows ? (g < kLaForget ? kLaForget : g) : 0.f;
-  double p = (double)g0;
+  double p = (double)g0 * 1.4426950408889634;
   p += la_dpp<0x111>(p);  // row_shr 1, 2, 4, 8
   p += la_dpp<0x112>(p);
   p += la_dpp<0x114>(p);
@@ -108,87 +120,133 @@ __device__ __forceinline__ float la_tables(float g, int rows, LaTab& t, int lane
   const float m1 = i < 1 ? b1 : 0.f, m2 = i < 2 ? b2 : 0.f, m3 = i < 3 ? b3 : 0.f;
   const float r1 = rest, r2 = r1 + m1, r3 = r2 + m2;  // from the row to the blocks behind its own
   t.p[lane] = p;
-  t.L[lane] = la_ex(pf);
-  t.E[lane] = scale * la_ex(before + pf);
-  t.T[lane] = la_ex(r3 + m3);
-  t.R[0][lane] = la_ex(r1);  // to block 1: read for rows of block 0
-  t.R[1][lane] = la_ex(r2);  // to block 2: of blocks 0, 1
-  t.R[2][lane] = la_ex(r3);
-  if (lane == 0) t.eC = la_ex((b0 + b1) + (b2 + b3));
+  t.L[lane] = scale * ex2(pf);
+  t.E[lane] = scale * ex2(before + pf);
+  t.T[lane] = ex2(r3 + m3);
+  t.R[0][lane] = ex2(r1);  // to block 1: read for rows of block 0
+  t.R[1][lane] = ex2(r2);  // to block 2: of blocks 0, 1
+  t.R[2][lane] = ex2(r3);
+  if (lane == 0) t.eC = ex2((b0 + b1) + (b2 + b3));
   return g0;
 }
 
 // ---- memory ----------------------------------------------------------------
-// The rows of a chunk as a buffer: a load past its last row gives zero, a store there is
-// dropped, and a lane's offsets are the same for every chunk (the base moves in scalar
-// registers).
 typedef unsigned u2v __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t la_buf(const void* p, size_t bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)(unsigned)bytes, 0x00020000);
 }
-// byte offset of (row, byte b) under a row stride; one past 32 bits stays out of range
-__device__ __forceinline__ unsigned la_off(int row, size_t stride, int b) {
-  const size_t x = (size_t)row * stride + b;
-  return x < 0xfffffff0u ? (unsigned)x : 0xfffffff0u;
-}
-__device__ __forceinline__ void la_put4(__amdgpu_buffer_rsrc_t buf, unsigned at, const f4& x) {
-  bf4 v;
-  v[0] = (__bf16)x[0], v[1] = (__bf16)x[1], v[2] = (__bf16)x[2], v[3] = (__bf16)x[3];
-  __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u2v, v), buf, at, 0, 0);
-}
-__device__ __forceinline__ void la_putf(__amdgpu_buffer_rsrc_t buf, unsigned at, const f4& x) {
-  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4v, x), buf, at, 0, 0);
-}
+
+// The rows of a segment from a chunk's first on, as a buffer: a load past the last row gives
+// zero, a store there is dropped, and a lane's offsets are the same for every chunk (what moves
+// is in scalar registers).  A segment spans at most 2^31 bytes (the call cuts it so).
+template <bool REV>
+struct LaRows {
+  const char* p;
+  unsigned left;
+  __device__ __forceinline__ LaRows(const void* base, unsigned stride, int width, int len) {
+    const int first = REV ? (len - 1) / CH : 0;  // the chunk a scan begins with
+    p = static_cast<const char*>(base) + (size_t)first * CH * stride;
+    left = (len - first * CH - 1) * stride + width;
+  }
+  __device__ __forceinline__ void next(unsigned stride) {
+    const unsigned step = CH * stride;
+    if (REV)
+      p -= step, left += step;
+    else
+      p += step, left -= step;
+  }
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t buf() const { return la_buf(p, left); }
+};
 
 // The log-decay of row `lane` of a chunk as it lies in memory: loaded a step before it is
 // needed, and looked at only there.
 struct LaDecays {
   const char* base;
-  size_t stride;  // bytes a row; 0: one for every token
+  unsigned stride;  // bytes a row; 0: one for every token
   unsigned off;
   __device__ __forceinline__ LaDecays(const LaGeo& a, size_t row0, int h, int lane) {
     base = reinterpret_cast<const char*>(a.per_head ? a.g + h : a.g + row0 * a.H + h);
-    stride = a.per_head ? 0 : (size_t)a.H * 4;
-    off = la_off(lane, stride, 0);
+    stride = a.per_head ? 0 : 4u * a.H;
+    off = lane * stride;
   }
   __device__ __forceinline__ float load(int chunk, int rows) const {
-    const auto buf = la_buf(base + (size_t)chunk * CH * stride, (size_t)(rows - 1) * stride + 4);
+    const auto buf = la_buf(base + (size_t)chunk * CH * stride, (rows - 1) * stride + 4);
     return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buf, off, 0, 0));
   }
 };
 
 // ---- tiles -----------------------------------------------------------------
-// COLS columns of 64 rows.  LDS row stride COLS + 8: the 16 rows that a fragment read touches
-// start in different banks; + 16 where the transposed reads are the most (four rows of 32
-// bytes at a time: 4 banks apart they would overlap).
-template <int COLS, int NTHR, int PAD = 8>
-struct LaTile {
-  static constexpr int LD = COLS + PAD, BYTES = CH * LD * 2;
-  static constexpr int PR = COLS / 8;                           // 16-byte pieces a row
-  static constexpr int NP = (CH * PR + NTHR - 1) / NTHR;        // pieces a thread
-  u4v x[NP];
-  struct Off {  // a thread's pieces in memory
-    unsigned at[NP];
-    __device__ __forceinline__ Off(size_t stride, int tid) {  // stride: bytes a row
+// 64 rows in LDS, 64 columns a plane, the 16-byte pieces of a row exchanged by piece ^ f(row),
+// f of the row in its block of 16.  Two ways of reading share the banks: 16-byte fragments
+// (which the LDS serves in groups of 16 lanes, rows 0-3 and 12-15 of one piece with rows 4-11
+// of the next), and transposed ones (4 rows, every other 8 of 64 bytes).  f keeps both free of
+// conflicts, 4 cycles a wave's instruction, where rows padded by 16 bytes took 8 and 4.
+// Planes lie apart by a constant that instructions hold, so that few addresses are formed.
+constexpr int kLaRow = 128, kLaPlane = CH * kLaRow;  // bytes
+constexpr int la_bytes(int cols) { return cols / 64 * kLaPlane; }
+__device__ __forceinline__ int la_swz(int row) { return ((row & 2) << 1) ^ ((row & 4) >> 1) ^ ((row & 8) ? 3 : 0); }
+
+// A lane's byte addresses inside a tile
+struct LaAt {
+  int frag;   // row c, columns 8 g ..; ^ 64: 32 columns on
+  int tr[2];  // transposed: rows 8 g + (c >> 2), and 4 on, columns 8 (c & 3) .. + 3; 8 on: the next four; ^ 64: 32 columns on
+  int z[2];   // the same of the wave's 32 columns
+  int out;    // row c, columns 8 g .. of the wave's
+  __device__ __forceinline__ LaAt(int lane, int wave) {
+    const int g = lane >> 4, c = lane & 15, mine = (wave >> 1) * kLaPlane, half = 64 * (wave & 1);
+    frag = c * kLaRow + ((g ^ la_swz(c)) << 4);
+    out = mine + (frag ^ half);
 #pragma unroll
-      for (int m = 0; m < NP; ++m) {
-        const int e = tid + m * NTHR;
-        at[m] = e < CH * PR ? la_off(e / PR, stride, 16 * (e % PR)) : 0xfffffff0u;
-      }
-    }
-  };
-  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t buf, const Off& off) {
-#pragma unroll
-    for (int m = 0; m < NP; ++m) x[m] = __builtin_amdgcn_raw_buffer_load_b128(buf, off.at[m], 0, 0);
-  }
-  __device__ __forceinline__ void store(__bf16* dst, int tid) const {
-#pragma unroll
-    for (int m = 0; m < NP; ++m) {
-      const int e = tid + m * NTHR;
-      if (CH * PR % NTHR == 0 || e < CH * PR) sts16(dst + e / PR * LD + 8 * (e % PR), x[m]);
+    for (int k = 0; k < 2; ++k) {
+      const int r = 8 * g + (c >> 2) + 4 * k;
+      tr[k] = r * kLaRow + (((c & 3) ^ la_swz(r)) << 4);
+      z[k] = mine + (tr[k] ^ half);
     }
   }
 };
+__device__ __forceinline__ bf8 la_ld16(const unsigned char* p) { return *reinterpret_cast<const bf8*>(p); }
+// Transposed fragment: rows 8 g + e of column c, from the two addresses of a lane
+__device__ __forceinline__ bf8 la_ld_tr(const unsigned char* p0, const unsigned char* p1) {
+  return ld_tr8p(reinterpret_cast<const __bf16*>(p0), reinterpret_cast<const __bf16*>(p1));
+}
+
+// A tile's way from memory straight into LDS, a kilobyte (8 rows of a plane) an instruction,
+// shared out over NW waves.  Rows past the segment's end become zero (the buffer's range).
+// Written out, and waited for with la_landed: as builtins, the compiler would hold every LDS
+// read behind them.
+template <int COLS, int NW>
+struct LaLoad {
+  static constexpr int NP = la_bytes(COLS) / 1024 / NW;  // instructions a wave, all of one plane
+  static_assert(NP % 2 == 0 && NP <= 8, "whole blocks of 16 rows in one plane");
+  unsigned off;
+  __device__ __forceinline__ LaLoad(unsigned stride, int lane, int wave) {  // stride: bytes a row, a multiple of 128
+    const int k = wave * NP;
+    off = (k / 8) * kLaRow + (8 * (k % 8) + lane / 8) * stride + (((lane % 8) ^ la_swz(lane / 8)) << 4);
+  }
+  template <bool REV>
+  __device__ __forceinline__ void load(const LaRows<REV>& r, unsigned stride, unsigned lds, int wave) const {
+    const u4v buf = {(unsigned)(uintptr_t)r.p, (unsigned)((uintptr_t)r.p >> 32) & 0xffffu, r.left, 0x00020000u};
+#pragma unroll
+    for (int m = 0; m < NP; ++m) {
+      const unsigned from = (off ^ (m & 1 ? 0x30 : 0)) + 8 * m * stride, at = lds + (wave * NP + m) * 1024;  // f(8) = 3
+      asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(from), "s"(buf) : "memory");
+    }
+  }
+};
+// All but the wave's last `after` memory instructions are done (they complete in order).
+template <int AFTER>
+__device__ __forceinline__ void la_landed() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(AFTER) : "memory");
+}
+// What lanes of a wave leave for each other in LDS: it serves a wave's instructions in order.
+__device__ __forceinline__ void la_wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+__device__ __forceinline__ unsigned la_lds(const void* p) {
+  return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
 
 // ---- splits ----------------------------------------------------------------
 // x = hi + lo (+ lower), bf16 parts of two values at a time.  What a part leaves is
@@ -231,142 +289,184 @@ __device__ __forceinline__ LaFr<PARTS> la_split8(const float (&x)[8]) {
   }
   return f;
 }
-__device__ __forceinline__ void la_split4(__bf16* hi, __bf16* lo, const f4& x) {
+template <int PARTS>
+__device__ __forceinline__ void la_split4(__bf16* p, int plane, const f4& x) {
   float r[4] = {x[0], x[1], x[2], x[3]};
-  const bf2 h0 = la_part(r[0], r[1]), h1 = la_part(r[2], r[3]);
-  la_left(h0, r[0], r[1]);
-  la_left(h1, r[2], r[3]);
-  const bf2 l0 = la_part(r[0], r[1]), l1 = la_part(r[2], r[3]);
-  *reinterpret_cast<bf4*>(hi) = bf4{h0[0], h0[1], h1[0], h1[1]};
-  *reinterpret_cast<bf4*>(lo) = bf4{l0[0], l0[1], l1[0], l1[1]};
+#pragma unroll
+  for (int k = 0; k < PARTS; ++k) {
+    const bf2 h0 = la_part(r[0], r[1]), h1 = la_part(r[2], r[3]);
+    *reinterpret_cast<bf4*>(p + k * plane) = bf4{h0[0], h0[1], h1[0], h1[1]};
+    if (k + 1 < PARTS) {
+      la_left(h0, r[0], r[1]);
+      la_left(h1, r[2], r[3]);
+    }
+  }
 }
 
-// X[r][..] fragment in the accumulators' row order: columns k0 + 4 g + (0..3), k0 + 16 + 4 g + (0..3)
-__device__ __forceinline__ bf8 ld_rows8(const __bf16* row, int k0, int g) {
-  const bf4 a = *reinterpret_cast<const bf4*>(row + k0 + 4 * g), b = *reinterpret_cast<const bf4*>(row + k0 + 16 + 4 * g);
-  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-}
-
-constexpr int LS = CH + 8;  // row stride of the score tiles (bf16)
-
-// ---- a wave's state: 16 columns over half of the A rows ---------------------
-// The two waves of a column group take the rows a0 .. a0 + A / 2 each: two waves a SIMD, which
-// hide each other's latencies (a wave with all of A: 325 us for the forward of B = 8, T = 4096,
-// 16 heads of 128 x 128, 10.8 thousand cycles a chunk of which 2.5 thousand issue).
+// ---- a wave's state: 32 columns over the A rows ------------------------------
+// Two blocks of 16: element m of block k is the wave's column 8 (m >> 2) + 4 k + (m & 3), so
+// that a lane's eight outputs of a row are eight columns side by side.  Rows likewise: element m
+// of block t is row 32 (t >> 1) + 8 (m >> 2) + 4 (t & 1) + (m & 3), and a lane's values of two
+// blocks are eight rows side by side, which meet 16 bytes of X.
 template <int A>
 struct LaState {
-  static constexpr int AH = A / 2;
-  f4 s[AH / 16];  // lane (g, c): rows a0 + 16 t + 4 g + u, column c
-  int a0;
+  f4 s[2][A / 16];  // lane (g, c): elements 4 g + u of block t, element c of block k
 
   __device__ __forceinline__ void zero() {
 #pragma unroll
-    for (int t = 0; t < AH / 16; ++t) s[t] = f4zero();
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int t = 0; t < A / 16; ++t) s[k][t] = f4zero();
   }
-  // row-major (A, ld), the wave's columns from c0 on; or its transpose, row-major (., A)
-  __device__ __forceinline__ void load(const float* src, int ld, int c0, int lane) {
-    const int g = lane >> 4, c = lane & 15;
+  __device__ __forceinline__ void decay(float eC) {
 #pragma unroll
-    for (int t = 0; t < AH / 16; ++t)
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
-      for (int u = 0; u < 4; ++u) s[t][u] = src[(size_t)(a0 + 16 * t + 4 * g + u) * ld + c0 + c];
+      for (int t = 0; t < A / 16; ++t) s[k][t] *= eC;
   }
-  __device__ __forceinline__ void load_t(const float* src, int c0, int lane) {
-    const int g = lane >> 4, c = lane & 15;
-#pragma unroll
-    for (int t = 0; t < AH / 16; ++t)
-      s[t] = *reinterpret_cast<const f4*>(src + (size_t)(c0 + c) * A + a0 + 16 * t + 4 * g);
+  // Row-major (A, LD), or with TR its transpose, row-major (LD, A).  One offset a lane, the rest
+  // in the instructions: sixty-four addresses would not fit.
+  template <int LD, bool TR>
+  __device__ __forceinline__ static unsigned at(int lane, int wave) {
+    const int g = lane >> 4, c = lane & 15, col = 32 * wave + 8 * (c >> 2) + (c & 3);
+    return 4 * (TR ? col * A + 8 * g : 8 * g * LD + col);
   }
-  __device__ __forceinline__ void store(float* dst, int ld, int c0, int lane) const {
-    const int g = lane >> 4, c = lane & 15;
+  template <int LD, bool TR>
+  __device__ __forceinline__ void load(const float* src, int lane, int wave) {
+    const auto buf = la_buf(src, A * LD * 4);
+    const unsigned off = at<LD, TR>(lane, wave);
 #pragma unroll
-    for (int t = 0; t < AH / 16; ++t)
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
-      for (int u = 0; u < 4; ++u) dst[(size_t)(a0 + 16 * t + 4 * g + u) * ld + c0 + c] = s[t][u];
+      for (int t = 0; t < A / 16; ++t) {
+        const int row = 32 * (t >> 1) + 4 * (t & 1);
+        if constexpr (TR) {
+          s[k][t] = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(buf, off + 4 * row, 16 * A * k, 0));
+        } else {
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            s[k][t][u] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buf, off + 4 * LD * u + 16 * k, 4 * LD * row, 0));
+        }
+      }
   }
-  __device__ __forceinline__ void store_t(float* dst, int c0, int lane) const {
-    const int g = lane >> 4, c = lane & 15;
+  template <int LD, bool TR>
+  __device__ __forceinline__ void store(float* dst, int lane, int wave) const {
+    const auto buf = la_buf(dst, A * LD * 4);
+    const unsigned off = at<LD, TR>(lane, wave);
 #pragma unroll
-    for (int t = 0; t < AH / 16; ++t)
-      *reinterpret_cast<f4*>(dst + (size_t)(c0 + c) * A + a0 + 16 * t + 4 * g) = s[t];
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int t = 0; t < A / 16; ++t) {
+        const int row = 32 * (t >> 1) + 4 * (t & 1);
+        const f4 x = s[k][t];
+        if constexpr (TR) {
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4v, x), buf, off + 4 * row, 16 * A * k, 0);
+        } else {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const float y = x[u];
+            __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(y), buf, off + 4 * LD * u + 16 * k, 4 * LD * row, 0);
+          }
+        }
+      }
   }
 
-  // acc[i] (columns c0 + 4 g + u of row 16 i + c) = X St over the wave's rows, the state split into PARTS
+  // acc[k][i] (elements 4 g + u of block k, row 16 i + c) = X St, the state split into PARTS; St <- eC St
   template <int PARTS>
-  __device__ __forceinline__ void read(const __bf16* X, int ld, f4 (&acc)[4], int lane) const {
-    const int g = lane >> 4, c = lane & 15;
+  __device__ __forceinline__ void read(const unsigned char* X, const LaAt& at, float eC, f4 (&acc)[2][4]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) acc[i] = f4zero();
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
-    for (int p = 0; p < AH / 32; ++p) {
-      const float x[8] = {s[2 * p][0],     s[2 * p][1],     s[2 * p][2],     s[2 * p][3],
-                          s[2 * p + 1][0], s[2 * p + 1][1], s[2 * p + 1][2], s[2 * p + 1][3]};
+      for (int i = 0; i < 4; ++i) acc[k][i] = f4zero();
+#pragma unroll
+    for (int p = 0; p < A / 32; ++p) {
+      const unsigned char* xp = X + (p >> 1) * kLaPlane + (at.frag ^ (64 * (p & 1)));
       bf8 b[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) b[i] = ld_rows8(X + (16 * i + c) * ld + a0, 32 * p, g);
-      const LaFr<PARTS> f = la_split8<PARTS>(x);
+      for (int i = 0; i < 4; ++i) b[i] = la_ld16(xp + 16 * i * kLaRow);
 #pragma unroll
-      for (int k = PARTS - 1; k >= 0; --k)
+      for (int k = 0; k < 2; ++k) {
+        float x[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] = mma(f.p[k], b[i], acc[i]);
+        for (int e = 0; e < 8; ++e) {
+          float z = s[k][2 * p + e / 4][e % 4];
+          const float y = z * eC;
+          asm("" : "+v"(z) : "v"(y));  // the decayed value lies elsewhere: the split takes this one's place
+          s[k][2 * p + e / 4][e % 4] = y;
+          x[e] = z;
+        }
+        const LaFr<PARTS> f = la_split8<PARTS>(x);
+#pragma unroll
+        for (int q = PARTS - 1; q >= 0; --q)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[k][i] = mma(f.p[q], b[i], acc[k][i]);
+      }
     }
   }
 
-  // St <- eC St + Y^T (w Z): z[kb] the wave's Z columns, rows 32 kb + 8 g + e
-  __device__ __forceinline__ void update(const __bf16* Y, int ld, const bf8 (&z)[2], const float* w, float eC, int lane) {
+  // St <- St + Y^T (w Z), w Z split into PARTS: z[k][kb] block k of the wave's Z columns, rows 32 kb + 8 g + e
+  template <int PARTS>
+  __device__ __forceinline__ void update(const unsigned char* Y, const LaAt& at, const bf8 (&z)[2][2], const float* w, int lane) {
     const int g = lane >> 4;
-    LaFr<3> d[2];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
-      float x[8], wv[8];
-      unpack8(z[kb], x);
+      float wv[8];
       ldf8(w + 32 * kb + 8 * g, wv);
+      LaFr<PARTS> d[2];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] *= wv[e];
-      d[kb] = la_split8<3>(x);
-    }
+      for (int k = 0; k < 2; ++k) {
+        float x[8];
+        unpack8(z[k][kb], x);
 #pragma unroll
-    for (int t = 0; t < AH / 16; ++t) s[t] *= eC;
+        for (int e = 0; e < 8; ++e) x[e] *= wv[e];
+        d[k] = la_split8<PARTS>(x);
+      }
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      bf8 y[AH / 16];
+      for (int t0 = 0; t0 < A / 16; t0 += 4) {
+        const unsigned char* yk = Y + 32 * kb * kLaRow + (t0 >> 2) * kLaPlane;
+        bf8 y[4];
 #pragma unroll
-      for (int t = 0; t < AH / 16; ++t) y[t] = ld_tr8(Y, ld, 32 * kb, a0 + 16 * t, lane);
+        for (int t = 0; t < 4; ++t) y[t] = la_ld_tr(yk + (at.tr[0] ^ (64 * (t >> 1))) + 8 * (t & 1), yk + (at.tr[1] ^ (64 * (t >> 1))) + 8 * (t & 1));
 #pragma unroll
-      for (int k = 2; k >= 0; --k)
+        for (int q = PARTS - 1; q >= 0; --q)
 #pragma unroll
-        for (int t = 0; t < AH / 16; ++t) s[t] = mma(y[t], d[kb].p[k], s[t]);
+          for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) s[k][t0 + t] = mma(y[t], d[k].p[q], s[k][t0 + t]);
+      }
     }
   }
 };
 
-// The two halves' X St meet in LDS: of the four row tiles the wave of half 0 keeps 0 and 3, the
-// other 1 and 2 (the same number of score tiles each way), and hands over the rest; 512 floats a wave.
-__device__ __forceinline__ void la_hand(const f4 (&acc)[4], bool hf, float* mine, int lane) {
-  *reinterpret_cast<f4*>(mine + 4 * lane) = hf ? acc[0] : acc[1];
-  *reinterpret_cast<f4*>(mine + 256 + 4 * lane) = hf ? acc[3] : acc[2];
-}
-__device__ __forceinline__ void la_take(const f4 (&acc)[4], bool hf, const float* other, f4 (&own)[2], int lane) {
-  own[0] = (hf ? acc[1] : acc[0]) + *reinterpret_cast<const f4*>(other + 4 * lane);
-  own[1] = (hf ? acc[2] : acc[3]) + *reinterpret_cast<const f4*>(other + 256 + 4 * lane);
+// Z fragments of the wave's columns, rows 32 kb + 8 g + e
+__device__ __forceinline__ void la_zfrags(const unsigned char* Z, const LaAt& at, bf8 (&z)[2][2]) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      const unsigned char* zk = Z + 32 * kb * kLaRow + 8 * k;
+      z[k][kb] = la_ld_tr(zk + at.z[0], zk + at.z[1]);
+    }
 }
 
 // ---- scores ----------------------------------------------------------------
-// One 16 x 16 tile of  sum_a Am[m][a] Bn[n][a]; lane (g, c): rows 4 g + u of Am, row c of Bn
-template <int A, int LDA, int LDB>
-__device__ __forceinline__ f4 la_score(const __bf16* Am, const __bf16* Bn, int m0, int n0, int lane) {
-  const int g = lane >> 4, c = lane & 15;
+// One 16 x 16 tile of  sum_a Am[16 mi + m][a] Bn[16 ni + n][a]; lane (g, c): rows 4 g + u of Am, row c of Bn
+template <int A>
+__device__ __forceinline__ f4 la_score(const unsigned char* Am, const unsigned char* Bn, const LaAt& at, int mi, int ni) {
+  const unsigned char *a = Am + 16 * mi * kLaRow, *b = Bn + 16 * ni * kLaRow;
   f4 x = f4zero();
 #pragma unroll
-  for (int p = 0; p < A / 32; ++p)
-    x = mma(ld8(Am + (m0 + c) * LDA + 32 * p + 8 * g), ld8(Bn + (n0 + c) * LDB + 32 * p + 8 * g), x);
+  for (int p = 0; p < A / 32; ++p) {
+    const int o = (p >> 1) * kLaPlane, f = at.frag ^ (64 * (p & 1));
+    x = mma(la_ld16(a + f + o), la_ld16(b + f + o), x);
+  }
   return x;
 }
 
-// Factors D_rs of a tile: ROWS of the lane's four values are s (r = r0 + c, one a lane), or r
-// (s = s0 + c).  i, j: the blocks of r and s.
+// Factors scale D_rs of a tile: ROWS_S, the lane's four values are s (r = r0 + c, one a lane), else
+// r (s = s0 + c).  i, j: the blocks of r and s; on the diagonal itself D is 1.
 template <bool ROWS_S>
-__device__ __forceinline__ f4 la_decay_tile(const LaTab& t, int i, int j, int lane) {
+__device__ __forceinline__ f4 la_decay_tile(const LaTab& t, int i, int j, int lane, float scale) {
   const int g = lane >> 4, c = lane & 15;
   f4 d;
   if (i != j) {
@@ -382,30 +482,32 @@ __device__ __forceinline__ f4 la_decay_tile(const LaTab& t, int i, int j, int la
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const double pu = t.p[16 * i + 4 * g + u];
-      const float e = la_ex((float)(ROWS_S ? pc - pu : pu - pc));
+      const float e = scale * ex2((float)(ROWS_S ? pc - pu : pu - pc));
       d[u] = (ROWS_S ? 4 * g + u <= c : c <= 4 * g + u) ? e : 0.f;
     }
   }
   return d;
 }
 
-__device__ __forceinline__ void la_zero_tile(__bf16* P, int r0, int s0, int lane) {
-  *reinterpret_cast<bf4*>(P + (r0 + (lane & 15)) * LS + s0 + 4 * (lane >> 4)) = bf4{};
-}
-
-// The lower tiles (i, j <= i) of a chunk's scores over the waves.  Eight waves: four take one on
-// the diagonal (dearer), three two off it, the last one the decays of the next chunk.  Twelve or
-// sixteen: one each, and the last wave the decays.
+// The lower tiles (i, j <= i) of a chunk's scores over the waves, fewer for the last, which forms
+// the decays of the next chunk.
 template <int NW>
-__device__ __forceinline__ int la_tiles(int wave) {
-  return NW == 8 ? (wave < 4 ? 1 : wave < 7 ? 2 : 0) : (wave < 10 ? 1 : 0);
-}
+__device__ __forceinline__ int la_tiles(int wave) { return NW == 4 ? (wave < 3 ? 3 : 1) : (wave < 1 ? 6 : 4); }
 template <int NW>
 __device__ __forceinline__ void la_tile_of(int wave, int m, int& i, int& j) {
-  // (0,0) (1,1) (2,2) (3,3) (3,0) (3,1) (3,2) (2,0) (2,1) (1,0)
-  const int n = NW == 8 && wave >= 4 ? 2 * wave - 4 + m : wave;
-  i = n < 4 ? n : n < 7 ? 3 : n < 9 ? 2 : 1;
-  j = n < 4 ? n : n < 7 ? n - 4 : n < 9 ? n - 7 : 0;
+  const int n = (NW == 4 ? 3 : 6) * wave + m;  // (3,0) (3,1) (3,2) (2,0) (2,1) (1,0) (0,0) (1,1) (2,2) (3,3)
+  i = n < 3 ? 3 : n < 5 ? 2 : n < 6 ? 1 : n - 6;
+  j = n < 3 ? n : n < 5 ? n - 3 : n < 6 ? 0 : n - 6;
+}
+
+// Score tiles in LDS, 512 bytes each (16 rows of the output, 16 columns that the product with Z
+// sums over): twelve a plane, so that the two tiles of a product over 32 columns lie side by
+// side, with a tile of zeros where that reaches past the diagonal.
+constexpr int kLaScores = 12 * 256;  // bf16 elements a plane
+template <bool REV>
+__device__ __forceinline__ int la_ptile(int i, int j) {  // row tile i, column tile j
+  if constexpr (REV) return i < 2 ? 4 * i + j : 2 * i + 2 + j;  // (i, j): 0 (0,0..3)  4 (1,0..3)  8 (2,2) (2,3)  10 (3,2) (3,3)
+  return i < 2 ? 2 * i + j : 4 * (i - 1) + j;                   // 0 (0,0) (0,1)  2 (1,0) (1,1)  4 (2,0..3)  8 (3,0..3)
 }
 
 }  // namespace
@@ -414,77 +516,71 @@ __device__ __forceinline__ void la_tile_of(int wave, int m, int& i, int& j) {
 // N = sum of Y^T (w Z) over the segment, from zero: S (k, v; first chunk to last) or, REV, dS
 // (q, dout; last to first).  Not needed of the segment that ends its chain.
 template <int DK, int DV, bool REV>
-__global__ __launch_bounds__(512) void la_segstate_kernel(LaScanArgs a) {
-  constexpr int NS = DV / 64, NTHR = 512, TW = 7;
-  using TY = LaTile<DK, NTHR, 16>;
-  using TZ = LaTile<64, NTHR>;
-  constexpr int BUF = TY::BYTES + TZ::BYTES;
-  __shared__ __align__(16) unsigned char smem[2 * BUF];
-  __shared__ LaTab tab[2];
+__global__ __launch_bounds__(2 * DV, 2) void la_segstate_kernel(LaScanArgs a) {
+  constexpr int NW = DV / 32, TW = NW - 1;
+  constexpr int OFF_Z = la_bytes(DK), BUF = OFF_Z + la_bytes(DV);
+  extern __shared__ __align__(16) unsigned char smem[];
+  LaTab* tab = reinterpret_cast<LaTab*>(smem + 2 * BUF);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int H = a.geo.H, HK = H / a.geo.G;
-  int unit, slice;
-  if (!la_slot<NS>(blockIdx.x, a.segs.nslot * H, unit, slice)) return;
+  const int unit = blockIdx.x;
   LaUnit un;
   if (!la_unit(a.segs, a.geo.T, unit / H, un)) return;
   if (REV ? un.first : un.last) return;
   const int h = unit % H, hk = h / a.geo.G;
   const int nc = (un.len + CH - 1) / CH;
-  const size_t sy = (size_t)HK * DK * 2, sz = (size_t)H * DV * 2;  // bytes a row
-  const bf16_t* Y = (REV ? a.q : a.k) + (un.row0 * HK + hk) * DK;
-  const bf16_t* Z = (REV ? a.dout : a.v) + (un.row0 * H + h) * DV + 64 * slice;
+  const unsigned sy = 2u * HK * DK, sz = 2u * H * DV;  // bytes a row
+  LaRows<REV> Y((REV ? a.q : a.k) + (un.row0 * HK + hk) * DK, sy, 2 * DK, un.len);
+  LaRows<REV> Z((REV ? a.dout : a.v) + (un.row0 * H + h) * DV, sz, 2 * DV, un.len);
   const float scale = REV ? a.geo.scale : 1.f;
   const auto at = [&](int n) { return REV ? nc - 1 - n : n; };
   const auto rows = [&](int n) { return min(CH, un.len - CH * at(n)); };
   const LaDecays decays(a.geo, un.row0, h, lane);
   const auto decay = [&](int n) { return decays.load(at(n), rows(n)); };
-  const auto sYb = [&](int n) { return reinterpret_cast<__bf16*>(smem + (n & 1) * BUF); };
-  const auto sZb = [&](int n) { return reinterpret_cast<__bf16*>(smem + (n & 1) * BUF + TY::BYTES); };
+  const unsigned lds = la_lds(smem);
+  const LaLoad<DK, NW> ly(sy, lane, wave);
+  const LaLoad<DV, NW> lz(sz, lane, wave);
+  const auto fetch = [&](int n) {
+    const unsigned to = lds + (n & 1) * BUF;
+    ly.load(Y, sy, to, wave);
+    lz.load(Z, sz, to + OFF_Z, wave);
+    Y.next(sy);
+    Z.next(sz);
+  };
+  const LaAt ay(lane, wave);
   double gs = 0.0;
   LaState<DK> st;
-  st.a0 = wave >= 4 ? DK / 2 : 0;
   st.zero();
-  TY ty;
-  TZ tz;
-  const typename TY::Off oy(sy, tid);
-  const typename TZ::Off oz(sz, tid);
-  const auto fetch = [&](int n) {
-    ty.load(la_buf(reinterpret_cast<const char*>(Y) + (size_t)(CH * at(n)) * sy, (rows(n) - 1) * sy + 2 * DK), oy);
-    tz.load(la_buf(reinterpret_cast<const char*>(Z) + (size_t)(CH * at(n)) * sz, (rows(n) - 1) * sz + 128), oz);
-  };
   float graw = 0.f;
   if (nc > 0) {
-    fetch(0);
     if (wave == TW) {
-      gs += (double)la_tables(decay(0), rows(0), tab[0], lane, scale);
+      graw = decay(0);
+      gs += (double)la_tables(graw, rows(0), tab[0], lane, scale);
       if (nc > 1) graw = decay(1);
     }
-    ty.store(sYb(0), tid);
-    tz.store(sZb(0), tid);
+    fetch(0);
   }
   for (int n = 0; n < nc; ++n) {
+    la_landed<0>();
     __syncthreads();
     const bool more = n + 1 < nc;
     if (more) {
-      fetch(n + 1);
       if (wave == TW) {
         gs += (double)la_tables(graw, rows(n + 1), tab[(n + 1) & 1], lane, scale);
         if (n + 2 < nc) graw = decay(n + 2);
       }
+      fetch(n + 1);
     }
     const LaTab& t = tab[n & 1];
-    const __bf16* sZ = sZb(n);
-    const int c0 = 16 * (wave & 3);
-    const bf8 z[2] = {ld_tr8(sZ, TZ::LD, 0, c0, lane), ld_tr8(sZ, TZ::LD, 32, c0, lane)};
-    st.update(sYb(n), TY::LD, z, REV ? t.E : t.T, t.eC, lane);
-    if (more) {
-      ty.store(sYb(n + 1), tid);
-      tz.store(sZb(n + 1), tid);
-    }
+    const unsigned char *sY = smem + (n & 1) * BUF, *sZ = sY + OFF_Z;
+    bf8 z[2][2];
+    la_zfrags(sZ, ay, z);
+    st.decay(t.eC);
+    st.template update<3>(sY, ay, z, REV ? t.E : t.T, lane);
   }
   float* N = (REV ? a.dS : a.S) + (size_t)unit * (DK * DV);
-  st.store(N, DV, 64 * slice + 16 * (wave & 3), lane);
-  if (slice == 0 && wave == TW) {
+  st.template store<DV, false>(N, lane, wave);
+  if (wave == TW) {
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) gs += __shfl_xor(gs, o);
     if (lane == 0) a.dec[unit] = la_ex((float)gs);
@@ -494,7 +590,7 @@ __global__ __launch_bounds__(512) void la_segstate_kernel(LaScanArgs a) {
 // The states behind the segments (rev: the gradients before them), in the place of their
 // contributions: what the chain's next segment starts from.
 __global__ __launch_bounds__(256) void la_segcombine_kernel(LaScanArgs a, int size, int rev) {
-  constexpr int AHEAD = 4;
+  constexpr int AHEAD = 8;
   const int H = a.geo.H, per = size / 1024;
   const int q = blockIdx.x / per, e = ((blockIdx.x % per) * 256 + threadIdx.x) * 4, s = q / H, h = q % H;
   int c0 = s * a.segs.nseg, c1 = c0 + a.segs.nseg;
@@ -528,445 +624,308 @@ __global__ __launch_bounds__(256) void la_segcombine_kernel(LaScanArgs a, int si
   }
 }
 
-// ---- o, and dq -------------------------------------------------------------
-// DQ false: o from q, k, v.  DQ true: dq from dout, v, k, with a_r and S at the anchors.
-// Two barriers a chunk: the tiles of the next one go to LDS beside this one's.
-template <int DK, int DV, bool DQ>
-struct LaFwdCfg {
-  static constexpr int A = DQ ? DV : DK, B = DQ ? DK : DV, NS = B / 64, NTHR = 512;
-  using TX = LaTile<A, NTHR>;
-  using TY = LaTile<A, NTHR, 16>;
-  using TZ = LaTile<64, NTHR>;
-  static constexpr int OFF_Y = TX::BYTES, OFF_Z = OFF_Y + TY::BYTES, BUF = OFF_Z + TZ::BYTES;
-  static constexpr int OFF_P = 2 * BUF, OFF_T = OFF_P + 2 * CH * LS * 2, OFF_X = OFF_T + 2 * (int)sizeof(LaTab);
-  static constexpr int OFF_A = OFF_X + 8 * 512 * 4;
-  static constexpr int LDS = OFF_A + (DQ ? 8 * CH * 4 : 0);
-  static_assert(LDS <= 160 * 1024, "LDS budget");
+// ---- the scans ---------------------------------------------------------------
+enum LaRole : int { kLaO, kLaDq, kLaDv, kLaDk };
+
+template <int DK, int DV, int ROLE>
+struct LaCfg {
+  static constexpr bool REV = ROLE == kLaDv || ROLE == kLaDk, TR = ROLE == kLaDq || ROLE == kLaDk;  // state transposed
+  static constexpr bool SUMS = ROLE == kLaDq || ROLE == kLaDv;  // gives a term of the decays' gradient
+  static constexpr int A = TR ? DV : DK, B = TR ? DK : DV, NW = B / 32;
+  // parts of the state and the scores in products, and of the decayed Z
+  static constexpr int PARTS = SUMS ? 3 : 2, UPARTS = ROLE == kLaDk ? 2 : 3;
+  static constexpr int OFF_Y = la_bytes(A), OFF_Z = 2 * OFF_Y, OFF_P = OFF_Z + la_bytes(B);
+  static constexpr int OFF_S = OFF_P + PARTS * kLaScores * 2, OFF_T = OFF_S + NW * 2048;
+  static constexpr int OFF_A = OFF_T + 2 * (int)sizeof(LaTab);
+  static constexpr int LDS = OFF_A + (SUMS ? (NW + 1) * CH * 4 + NW * 64 : 0);
+  static_assert(LDS <= 80 * 1024, "two workgroups a CU");
 };
 
-template <int DK, int DV, bool DQ>
-__device__ __forceinline__ void la_forward(const LaScanArgs& a, int block, unsigned char* smem) {
-  using C = LaFwdCfg<DK, DV, DQ>;
-  constexpr int A = C::A, B = C::B, TW = 7;
-  __bf16 *sPh = reinterpret_cast<__bf16*>(smem + C::OFF_P), *sPl = sPh + CH * LS;
+template <int DK, int DV, int ROLE>
+__device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned char* smem) {
+  using C = LaCfg<DK, DV, ROLE>;
+  constexpr int A = C::A, B = C::B, NW = C::NW, TW = NW - 1, PARTS = C::PARTS;
+  constexpr bool REV = C::REV, SUMS = C::SUMS, TR = C::TR;
+  const unsigned char *sX = smem, *sY = smem + C::OFF_Y, *sZ = smem + C::OFF_Z;
+  __bf16* sP = reinterpret_cast<__bf16*>(smem + C::OFF_P);
   LaTab* tab = reinterpret_cast<LaTab*>(smem + C::OFF_T);
-  float *sEx = reinterpret_cast<float*>(smem + C::OFF_X), *sA = reinterpret_cast<float*>(smem + C::OFF_A);
+  float *sA = reinterpret_cast<float*>(smem + C::OFF_A), *sDiag = sA + NW * CH, *sC = sDiag + CH;  // a wave's terms, the scores' diagonal, a wave's sums
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  if (wave >= NW) return;  // of a wider role beside this one
   const int g = lane >> 4, c = lane & 15;
-  const bool hf = wave >= 4;
   const int H = a.geo.H, HK = H / a.geo.G;
-  int unit, slice;
-  if (!la_slot<C::NS>(block, a.segs.nslot * H, unit, slice)) return;
   LaUnit un;
   if (!la_unit(a.segs, a.geo.T, unit / H, un)) return;
   const int h = unit % H, hk = h / a.geo.G, nc = (un.len + CH - 1) / CH;
-  const int b0 = 64 * slice + 16 * (wave & 3);                     // the wave's columns
-  const size_t sk = (size_t)HK * DK * 2, sv = (size_t)H * DV * 2;  // bytes a row
-  const bf16_t *k0 = a.k + (un.row0 * HK + hk) * DK, *v0 = a.v + (un.row0 * H + h) * DV;
-  const bf16_t* q0 = a.q + (un.row0 * HK + hk) * DK;
-  const bf16_t *X = DQ ? a.dout + (un.row0 * H + h) * DV : q0, *Y = DQ ? v0 : k0, *Z = (DQ ? k0 : v0) + 64 * slice;
-  const size_t sx = DQ ? sv : sk, sz = DQ ? sk : sv;
-  const auto chunk = [](const void* p, size_t stride, int n, int rows, int width) {
-    return la_buf(static_cast<const char*>(p) + (size_t)(CH * n) * stride, (size_t)(rows - 1) * stride + width);
-  };
-  const auto rows = [&](int n) { return min(CH, un.len - CH * n); };
-  const LaDecays decays(a.geo, un.row0, h, lane);
-  const auto decay = [&](int n) { return decays.load(n, rows(n)); };
-
-  LaState<A> st;
-  st.a0 = hf ? A / 2 : 0;
-  {
-    const float* init = un.first ? (a.S0 ? a.S0 + ((size_t)un.seq * H + h) * (DK * DV) : nullptr)
-                                 : a.S + ((size_t)unit - H) * (DK * DV);
-    if (init == nullptr)
-      st.zero();
-    else if (DQ)
-      st.load_t(init, b0, lane);
-    else
-      st.load(init, DV, b0, lane);
-  }
-  typename C::TX tx;
-  typename C::TY ty;
-  typename C::TZ tz;
-  const typename C::TX::Off ox(sx, tid);
-  const typename C::TY::Off oy(sx, tid);
-  const typename C::TZ::Off oz(sz, tid);
-  const auto fetch = [&](int n) {
-    tx.load(chunk(X, sx, n, rows(n), 2 * A), ox);
-    ty.load(chunk(Y, sx, n, rows(n), 2 * A), oy);
-    tz.load(chunk(Z, sz, n, rows(n), 128), oz);
-  };
-  const auto settle = [&](int buf) {
-    tx.store(reinterpret_cast<__bf16*>(smem + buf * C::BUF), tid);
-    ty.store(reinterpret_cast<__bf16*>(smem + buf * C::BUF + C::OFF_Y), tid);
-    tz.store(reinterpret_cast<__bf16*>(smem + buf * C::BUF + C::OFF_Z), tid);
-  };
-  // output rows 16 i + c, columns b0 + 4 g: a row each of o, dq or the group's part
-  const int i0 = hf ? 1 : 0, i1 = hf ? 2 : 3;  // the wave's row tiles
-  const bool part = DQ && a.Pq != nullptr;
-  const size_t so = DQ ? (part ? (size_t)H * DK * 4 : sk) : sv;
-  char* O = DQ ? (part ? reinterpret_cast<char*>(a.Pq + (un.row0 * H + h) * DK)
-                       : reinterpret_cast<char*>(a.dq + (un.row0 * HK + hk) * DK))
-               : reinterpret_cast<char*>(a.o + (un.row0 * H + h) * DV);
-  const unsigned oo[2] = {la_off(16 * i0 + c, so, (part ? 4 : 2) * (b0 + 4 * g)),
-                          la_off(16 * i1 + c, so, (part ? 4 : 2) * (b0 + 4 * g))};
-  unsigned oq[4];
-  if constexpr (DQ) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) oq[i] = la_off(16 * i + c, sk, 2 * (b0 + 4 * g));
-  }
-  float graw = 0.f;
-  if (nc > 0) {
-    fetch(0);
-    if (wave == TW) {
-      la_tables(decay(0), rows(0), tab[0], lane, 1.f);
-      if (nc > 1) graw = decay(1);
-    }
-    if (wave == 1) {  // the tiles above the diagonal that a product of 32 rows meets
-      la_zero_tile(sPh, 0, 16, lane);
-      la_zero_tile(sPl, 0, 16, lane);
-      la_zero_tile(sPh, 32, 48, lane);
-      la_zero_tile(sPl, 32, 48, lane);
-    }
-    settle(0);
-  }
-  const auto step = [&](int n, auto buf) {  // buf: n's parity
-    constexpr int BUF = decltype(buf)::value;
-    __syncthreads();
-    const bool more = n + 1 < nc;
-    const LaTab& t = tab[BUF];
-    const int len = rows(n);
-    const __bf16* sX = reinterpret_cast<const __bf16*>(smem + BUF * C::BUF);
-    const __bf16* sY = reinterpret_cast<const __bf16*>(smem + BUF * C::BUF + C::OFF_Y);
-    const __bf16* sZ = reinterpret_cast<const __bf16*>(smem + BUF * C::BUF + C::OFF_Z);
-    bf4 qv[4];
-    if constexpr (DQ) {
-      const auto buf = chunk(q0, sk, n, len, 2 * DK);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        qv[i] = __builtin_bit_cast(bf4, __builtin_amdgcn_raw_buffer_load_b64(buf, oq[i], 0, 0));
-    }
-    if (more) fetch(n + 1);
-    // scores, P[r][s], four s a lane
-#pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      if (m < la_tiles<8>(wave)) {
-        int i, j;
-        la_tile_of<8>(wave, m, i, j);
-        f4 x = la_score<A, C::TY::LD, C::TX::LD>(sY, sX, 16 * j, 16 * i, lane);
-        x *= la_decay_tile<true>(t, i, j, lane);
-        const int at = (16 * i + c) * LS + 16 * j + 4 * g;
-        la_split4(sPh + at, sPl + at, x);
-      }
-    }
-    if (more && wave == TW) {
-      la_tables(graw, rows(n + 1), tab[BUF ^ 1], lane, 1.f);
-      if (n + 2 < nc) graw = decay(n + 2);
-    }
-    f4 acc[4];
-    st.template read<DQ ? 3 : 2>(sX, C::TX::LD, acc, lane);
-    if constexpr (DQ) {
-      // a_r over the wave's columns and its half of the state
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float x = 0.f;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) x += acc[i][u] * (float)qv[i][u];
-        x += row_partner16(x, (lane & 16) != 0);
-        x += row_partner32(x, lane >= 32);
-        if (g == 0) sA[wave * CH + 16 * i + c] = x;
-      }
-    }
-    la_hand(acc, hf, sEx + wave * 512, lane);
-    __syncthreads();
-    f4 own[2];
-    la_take(acc, hf, sEx + (wave ^ 4) * 512, own, lane);
-    own[0] *= t.E[16 * i0 + c];
-    own[1] *= t.E[16 * i1 + c];
-    const int c0 = 16 * (wave & 3);
-    const bf8 z[2] = {ld_tr8(sZ, C::TZ::LD, 0, c0, lane), ld_tr8(sZ, C::TZ::LD, 32, c0, lane)};
-    const __bf16 *p0 = sPh + (16 * i0 + c) * LS + 8 * g, *p1 = sPh + (16 * i1 + c) * LS + 8 * g;
-    constexpr int PL = CH * LS;  // from the high plane to the low
-    own[0] = mma(z[0], ld8(p0 + PL), own[0]);
-    own[1] = mma(z[0], ld8(p1 + PL), own[1]);
-    own[0] = mma(z[0], ld8(p0), own[0]);
-    own[1] = mma(z[1], ld8(p1 + PL + 32), own[1]);
-    own[1] = mma(z[0], ld8(p1), own[1]);
-    own[1] = mma(z[1], ld8(p1 + 32), own[1]);
-    st.update(sY, C::TY::LD, z, t.T, t.eC, lane);
-    const float sc = a.geo.scale;
-    const size_t row = un.row0 + CH * n;
-    const auto out = chunk(O, so, n, len, (part ? 4 : 2) * B);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      if (part)
-        la_putf(out, oo[i], own[i] * sc);
-      else
-        la_put4(out, oo[i], own[i] * sc);
-    }
-    if constexpr (DQ) {
-      if ((n + 1) % kLaAnchor == 0 || !more)
-        st.store_t(a.aS + ((size_t)unit * a.anchors + n / kLaAnchor) * (DK * DV), b0, lane);
-      if (wave == 0 && lane < len) {
-        float x = 0.f;
-#pragma unroll
-        for (int w = 0; w < 8; ++w) x += sA[w * CH + lane];
-        a.pa[((size_t)slice * a.geo.B * a.geo.T + row + lane) * H + h] = sc * x * t.E[lane];
-      }
-    }
-    if (more) settle(BUF ^ 1);
-  };
-  for (int n = 0; n < nc; n += 2) {
-    step(n, std::integral_constant<int, 0>{});
-    if (n + 1 < nc) step(n + 1, std::integral_constant<int, 1>{});
-  }
-  if constexpr (!DQ) {
-    if (un.last && a.ST) st.store(a.ST + ((size_t)un.seq * H + h) * (DK * DV), DV, b0, lane);
-  }
-}
-
-template <int DK, int DV>
-__global__ __launch_bounds__(512) void la_scan_fwd_kernel(LaScanArgs a) {
-  extern __shared__ __align__(16) unsigned char smem[];
-  la_forward<DK, DV, false>(a, blockIdx.x, smem);
-}
-template <int DK, int DV>
-__global__ __launch_bounds__(512) void la_scan_dq_kernel(LaScanArgs a) {
-  extern __shared__ __align__(16) unsigned char smem[];
-  la_forward<DK, DV, true>(a, blockIdx.x, smem);
-}
-
-// ---- dk and dv -------------------------------------------------------------
-// A workgroup takes a slice of dv's columns (its first NWV waves) and one of dk's; both read
-// the same four tiles, of which LDS holds one chunk's at a time.
-template <int DK, int DV>
-struct LaRevCfg {
-  static constexpr int NS = (DK > DV ? DK : DV) / 64;
-  static constexpr int BV = DV / NS, BK = DK / NS, NWV = BV / 8, NWK = BK / 8, NW = NWV + NWK, NTHR = 64 * NW;
-  using TK = LaTile<DK, NTHR>;
-  using TQ = LaTile<DK, NTHR, 16>;
-  using TV = LaTile<DV, NTHR>;
-  using TD = LaTile<DV, NTHR, 16>;
-  static constexpr int OFF_K = TQ::BYTES, OFF_V = OFF_K + TK::BYTES, OFF_D = OFF_V + TV::BYTES, OFF_P = OFF_D + TD::BYTES;
-  static constexpr int PB = CH * LS * 2;  // one plane of scores
-  static constexpr int OFF_T = OFF_P + 4 * PB, OFF_X = OFF_T + 2 * (int)sizeof(LaTab), OFF_W = OFF_X + NW * 512 * 4;
-  static constexpr int LDS = OFF_W + (4 + 4 + NWV) * CH * 4;
-  static_assert(NW > 10 && LDS <= 160 * 1024, "a wave a score tile, one for the decays");
-};
-
-template <int DK, int DV, bool ISV>
-__device__ __forceinline__ void la_reverse(const LaScanArgs& a, unsigned char* smem) {
-  using C = LaRevCfg<DK, DV>;
-  constexpr int A = ISV ? DK : DV, NG = (ISV ? C::NWV : C::NWK) / 2, TW = 0;  // rows of the role's state, column groups
-  __bf16 *sQ = reinterpret_cast<__bf16*>(smem), *sK = reinterpret_cast<__bf16*>(smem + C::OFF_K);
-  __bf16 *sV = reinterpret_cast<__bf16*>(smem + C::OFF_V), *sD = reinterpret_cast<__bf16*>(smem + C::OFF_D);
-  __bf16* sP = reinterpret_cast<__bf16*>(smem + C::OFF_P);  // planes: q k hi, lo; do v hi, lo
-  LaTab* tab = reinterpret_cast<LaTab*>(smem + C::OFF_T);
-  float* sRow = reinterpret_cast<float*>(smem + C::OFF_W);  // [j][r], [i][s], [wave][s]
-  float *sCol = sRow + 4 * CH, *sB = sCol + 4 * CH, *sEx = reinterpret_cast<float*>(smem + C::OFF_X);
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int g = lane >> 4, c = lane & 15;
-  const int H = a.geo.H, HK = H / a.geo.G;
-  int unit, slice;
-  if (!la_slot<C::NS>(blockIdx.x, a.segs.nslot * H, unit, slice)) return;
-  LaUnit un;
-  if (!la_unit(a.segs, a.geo.T, unit / H, un)) return;
-  const int h = unit % H, hk = h / a.geo.G, nc = (un.len + CH - 1) / CH;
-  const size_t sk = (size_t)HK * DK * 2, sv = (size_t)H * DV * 2;  // bytes a row
-  const bf16_t *q0 = a.q + (un.row0 * HK + hk) * DK, *k0 = a.k + (un.row0 * HK + hk) * DK;
-  const bf16_t *v0 = a.v + (un.row0 * H + h) * DV, *d0 = a.dout + (un.row0 * H + h) * DV;
+  const unsigned sk = 2u * HK * DK, sv = 2u * H * DV;        // bytes a row
+  const unsigned sx = TR ? sv : sk, sz = TR ? sk : sv;       // of X and Y; of Z, the output and E
+  const size_t rk = (un.row0 * HK + hk) * DK, rv = (un.row0 * H + h) * DV;
+  const bf16_t *q0 = a.q + rk, *k0 = a.k + rk, *v0 = a.v + rv, *d0 = a.dout + rv;
+  // output: grouped heads' parts in fp32, a row for each value head, or bf16
+  float* part = ROLE == kLaDq ? a.Pq : ROLE == kLaDk ? a.Pk : nullptr;
+  const unsigned so = part ? 4u * H * DK : sz;
+  void* out0 = part ? (void*)(part + (un.row0 * H + h) * DK)
+                    : (void*)(ROLE == kLaO ? a.o + rv : ROLE == kLaDv ? a.dv + rv : (ROLE == kLaDq ? a.dq : a.dk) + rk);
+  LaRows<REV> X(ROLE == kLaO ? q0 : ROLE == kLaDq ? d0 : ROLE == kLaDv ? k0 : v0, sx, 2 * A, un.len);
+  LaRows<REV> Y(ROLE == kLaO ? k0 : ROLE == kLaDq ? v0 : ROLE == kLaDv ? q0 : d0, sx, 2 * A, un.len);
+  LaRows<REV> Z(ROLE == kLaO ? v0 : ROLE == kLaDq ? k0 : ROLE == kLaDv ? d0 : q0, sz, 2 * B, un.len);
+  LaRows<REV> E(ROLE == kLaDq ? q0 : v0, sz, 2 * B, un.len);  // what the output is multiplied with for the decays' gradient
+  LaRows<REV> out(out0, so, part ? 4 * B : 2 * B, un.len);
   const float scale = a.geo.scale;
-  const auto at = [&](int n) { return nc - 1 - n; };
+  const auto at = [&](int n) { return REV ? nc - 1 - n : n; };
   const auto rows = [&](int n) { return min(CH, un.len - CH * at(n)); };
   const LaDecays decays(a.geo, un.row0, h, lane);
   const auto decay = [&](int n) { return decays.load(at(n), rows(n)); };
-  const int rw = ISV ? wave : wave - C::NWV;  // wave of the role
-  const bool hf = rw >= NG;
-  const int b0 = (ISV ? C::BV : C::BK) * slice + 16 * (hf ? rw - NG : rw);
 
-  LaState<A> st;  // dS, columns of Dv; or dS^T, columns of Dk
-  st.a0 = hf ? A / 2 : 0;
+  LaState<A> st;
   {
-    const float* init = un.last ? (a.dST ? a.dST + ((size_t)un.seq * H + h) * (DK * DV) : nullptr)
-                                : a.dS + ((size_t)unit + H) * (DK * DV);
+    const float* given = REV ? a.dST : a.S0;
+    const float* init = (REV ? un.last : un.first) ? (given ? given + ((size_t)un.seq * H + h) * (DK * DV) : nullptr)
+                                                   : (REV ? a.dS + ((size_t)unit + H) * (DK * DV)
+                                                          : a.S + ((size_t)unit - H) * (DK * DV));
     if (init == nullptr)
       st.zero();
-    else if (ISV)
-      st.load(init, DV, b0, lane);
     else
-      st.load_t(init, b0, lane);
+      st.template load<B, TR>(init, lane, wave);
   }
-  typename C::TQ tq;
-  typename C::TK tk;
-  typename C::TV tv;
-  typename C::TD td;
-  const typename C::TQ::Off oq(sk, tid);
-  const typename C::TK::Off ok(sk, tid);
-  const typename C::TD::Off od(sv, tid);
-  const typename C::TV::Off ov(sv, tid);
-  const auto chunk = [&](const void* p, size_t stride, int n, int width) {
-    return la_buf(static_cast<const char*>(p) + (size_t)(CH * at(n)) * stride, (size_t)(rows(n) - 1) * stride + width);
-  };
-  const auto fetch = [&](int n) {
-    tq.load(chunk(q0, sk, n, 2 * DK), oq);
-    tk.load(chunk(k0, sk, n, 2 * DK), ok);
-    tv.load(chunk(v0, sv, n, 2 * DV), ov);
-    td.load(chunk(d0, sv, n, 2 * DV), od);
-  };
-  const auto settle = [&] {
-    tq.store(sQ, tid);
-    tk.store(sK, tid);
-    tv.store(sV, tid);
-    td.store(sD, tid);
-  };
-  const bool part = !ISV && a.Pk != nullptr;
-  const size_t so = ISV ? sv : part ? (size_t)H * DK * 4 : sk;
-  char* O = ISV ? reinterpret_cast<char*>(a.dv + (un.row0 * H + h) * DV)
-                : part ? reinterpret_cast<char*>(a.Pk + (un.row0 * H + h) * DK)
-                       : reinterpret_cast<char*>(a.dk + (un.row0 * HK + hk) * DK);
-  const int wo = ISV ? 2 * DV : (part ? 4 : 2) * DK;
-  const int i0 = hf ? 1 : 0, i1 = hf ? 2 : 3;  // the wave's row tiles
-  const unsigned oo[2] = {la_off(16 * i0 + c, so, (part ? 4 : 2) * (b0 + 4 * g)),
-                          la_off(16 * i1 + c, so, (part ? 4 : 2) * (b0 + 4 * g))};
+  const unsigned lds = la_lds(smem);
+  const LaLoad<A, NW> lx(sx, lane, wave);
+  const LaLoad<B, NW> lz(sz, lane, wave);
+  const LaAt ax(lane, wave);
+  // Rows of E and of the output in memory are four lanes' sixteen bytes (a quarter of the address
+  // cycles of a row a lane); they pass through the wave's own two kilobytes, 32 rows at a time.
+  const unsigned o0 = (lane >> 2) * sz + 64 * wave + 16 * (lane & 3);
+  unsigned char* sS = smem + C::OFF_S + 2048 * wave;
+  const int sm = 64 * (lane >> 2) + (((lane & 3) ^ (-(lane >> 4) & 3)) << 4);  // as in memory: row lane >> 2, piece lane & 3
+  const int sr = 64 * c + ((g ^ (-(c >> 2) & 3)) << 4);                        // as the products have it: row c, piece g
   float graw = 0.f;
   if (nc > 0) {
-    fetch(0);
     if (wave == TW) {
       la_tables(decay(0), rows(0), tab[0], lane, scale);
       if (nc > 1) graw = decay(1);
     }
-    if (wave == 1) {
+    if (wave == 0) {  // the tiles past the diagonal
 #pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        la_zero_tile(sP + m * (CH * LS), 16, 0, lane);
-        la_zero_tile(sP + m * (CH * LS), 48, 32, lane);
+      for (int k = 0; k < PARTS; ++k) {
+        *reinterpret_cast<bf4*>(sP + k * kLaScores + (REV ? la_ptile<REV>(1, 0) : la_ptile<REV>(0, 1)) * 256 + 4 * lane) = bf4{};
+        *reinterpret_cast<bf4*>(sP + k * kLaScores + (REV ? la_ptile<REV>(3, 2) : la_ptile<REV>(2, 3)) * 256 + 4 * lane) = bf4{};
       }
     }
-    settle();
+    lx.load(X, sx, lds, wave);
+    lz.load(Z, sz, lds + C::OFF_Z, wave);
+    la_landed<0>();
   }
+  // chunk n's terms over the waves, a barrier after they were left
+  const auto total = [&](int n) {
+    float x = sA[lane] + sA[CH + lane];
+    if (NW == 4) x += sA[2 * CH + lane] + sA[3 * CH + lane];
+    if (lane < rows(n)) (ROLE == kLaDq ? a.pa : a.pb)[(un.row0 + CH * at(n) + lane) * H + h] = x;
+    if (lane < 16) {
+      float y = sC[lane] + sC[16 + lane];
+      if (NW == 4) y += sC[32 + lane] + sC[48 + lane];
+      (ROLE == kLaDq ? a.ca : a.cb)[((size_t)unit * (a.segs.seg_tokens / CH) + at(n)) * 16 + lane] = y;
+    }
+  };
   for (int n = 0; n < nc; ++n) {
-    __syncthreads();
+    __syncthreads();  // X and Z are there; Y, P and the terms of the chunk before are done with
+    lx.load(Y, sx, lds + C::OFF_Y, wave);
+    Y.next(sx);
     const bool more = n + 1 < nc;
     const LaTab& t = tab[n & 1];
-    const int len = rows(n), cn = at(n);
-    const size_t row = un.row0 + CH * cn;
-    if (more) fetch(n + 1);
-    if constexpr (ISV) {
+    const int cn = at(n);
+    if constexpr (ROLE == kLaDv) {
       if ((cn + 1) % kLaAnchor == 0 || n == 0)  // dS behind this chunk
-        st.store(a.aD + ((size_t)unit * a.anchors + cn / kLaAnchor) * (DK * DV), DV, b0, lane);
+        st.template store<B, TR>(a.aD + ((size_t)unit * a.anchors + cn / kLaAnchor) * (DK * DV), lane, wave);
     }
-    // scores, P[s][r], four r a lane, and the sums of W
-    {
-      // the waves of dk take them (two parts of the state to dv's three), dv's first what is over
-      const int m = C::NW - 1 - wave;
-      if (m < 10) {
+    f4 acc[2][4];
+    st.template read<PARTS>(sX, ax, t.eC, acc);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float f = (REV ? t.T : t.E)[16 * i + c];
+      acc[0][i] *= f;
+      acc[1][i] *= f;
+    }
+    bf8 z[2][2];
+    la_zfrags(sZ, ax, z);
+    la_landed<0>();
+    __syncthreads();  // Y is there
+    u4v er[SUMS ? 4 : 1];
+    bf8 zr[SUMS ? 4 : 1];  // Z as the output lies
+    if constexpr (SUMS) {
+      if (wave == 0 && n > 0) total(n - 1);
+      const auto be = E.buf();
+      E.next(sz);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        er[i] = __builtin_amdgcn_raw_buffer_load_b128(be, o0 + 16 * i * sz, 0, 0);  // in L1 or L2 since the tiles' loads
+        zr[i] = la_ld16(sZ + ax.out + 16 * i * kLaRow);
+      }
+    }
+    // scores: rows of the output by rows of Z, four of the latter a lane
+#pragma unroll
+    for (int m = 0; m < la_tiles<NW>(0); ++m) {
+      if (m < la_tiles<NW>(wave)) {
         int i, j;
-        la_tile_of<C::NW>(m, 0, i, j);
-        const f4 d = la_decay_tile<false>(t, i, j, lane) * scale;
-        const f4 x = la_score<DK, C::TQ::LD, C::TK::LD>(sQ, sK, 16 * i, 16 * j, lane) * d;
-        const f4 y = la_score<DV, C::TD::LD, C::TV::LD>(sD, sV, 16 * i, 16 * j, lane);
-        const int p = (16 * j + c) * LS + 16 * i + 4 * g;
-        la_split4(sP + p, sP + CH * LS + p, x);
-        la_split4(sP + 2 * CH * LS + p, sP + 3 * CH * LS + p, y * d);
-        f4 w = x * y;
-        if (i == j) {
+        la_tile_of<NW>(wave, m, i, j);
+        const int io = REV ? j : i, jz = REV ? i : j;  // output's and Z's block
+        f4 x = la_score<A>(sY, sX, ax, jz, io);
+        x *= la_decay_tile<!REV>(t, i, j, lane, scale);
+        if constexpr (SUMS) {
+          // the diagonal cancels between a and b: it is kept out of both and added to the output by itself
+          if (i == j) {
 #pragma unroll
-          for (int u = 0; u < 4; ++u) w[u] = c < 4 * g + u ? w[u] : 0.f;
+            for (int u = 0; u < 4; ++u)
+              if (4 * g + u == c) {
+                sDiag[16 * i + c] = x[u];
+                x[u] = 0.f;
+              }
+          }
         }
-        float col = (w[0] + w[1]) + (w[2] + w[3]);
-        col += row_partner16(col, (lane & 16) != 0);
-        col += row_partner32(col, lane >= 32);
-        if (g == 0) sCol[i * CH + 16 * j + c] = col;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) w[u] = row_sum(w[u]);
-        if (c == 0) *reinterpret_cast<f4*>(&sRow[j * CH + 16 * i + 4 * g]) = w;
+        la_split4<PARTS>(sP + la_ptile<REV>(io, jz) * 256 + 16 * c + 4 * g, kLaScores, x);
       }
     }
     if (more && wave == TW) {
       la_tables(graw, rows(n + 1), tab[(n + 1) & 1], lane, scale);
       if (n + 2 < nc) graw = decay(n + 2);
     }
-    f4 acc[4];
-    st.template read<ISV ? 3 : 2>(ISV ? sK : sV, ISV ? C::TK::LD : C::TV::LD, acc, lane);
-    if constexpr (ISV) {
-      // b_s over the wave's columns and its half of the state
+    if constexpr (SUMS) {
+      // here, so that no wait for them stands behind the tiles' loads
+#pragma unroll
+      for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(er[i]));
+    }
+    __syncthreads();  // P is there; X and Z are done with
+    if (more) {
+      X.next(sx);
+      Z.next(sz);
+      lx.load(X, sx, lds, wave);
+      lz.load(Z, sz, lds + C::OFF_Z, wave);
+    }
+    bf8 ev[SUMS ? 4 : 1];
+    if constexpr (SUMS) {
+      float y = 0.f;  // what the state gives to a chunk's sum
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const bf4 vv = *reinterpret_cast<const bf4*>(sV + (16 * i + c) * C::TV::LD + b0 + 4 * g);
-        float x = 0.f;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) x += acc[i][u] * (float)vv[u];
-        x += row_partner16(x, (lane & 16) != 0);
-        x += row_partner32(x, lane >= 32);
-        if (g == 0) sB[wave * CH + 16 * i + c] = x;
-      }
-    }
-    la_hand(acc, hf, sEx + wave * 512, lane);
-    __syncthreads();
-    f4 own[2];
-    la_take(acc, hf, sEx + (hf ? wave - NG : wave + NG) * 512, own, lane);
-    own[0] *= t.T[16 * i0 + c];
-    own[1] *= t.T[16 * i1 + c];
-    const __bf16* Z = ISV ? sD : sQ;
-    constexpr int LDZ = ISV ? C::TD::LD : C::TQ::LD;
-    const bf8 z[2] = {ld_tr8(Z, LDZ, 0, b0, lane), ld_tr8(Z, LDZ, 32, b0, lane)};
-    const __bf16* Ph = sP + (ISV ? 0 : 2 * CH * LS);
-    const __bf16 *p0 = Ph + (16 * i0 + c) * LS + 8 * g, *p1 = Ph + (16 * i1 + c) * LS + 8 * g;
-    constexpr int PL = CH * LS;
-    own[0] = mma(z[0], ld8(p0 + PL), own[0]);
-    own[1] = mma(z[1], ld8(p1 + PL + 32), own[1]);
-    own[0] = mma(z[1], ld8(p0 + PL + 32), own[0]);
-    own[1] = mma(z[1], ld8(p1 + 32), own[1]);
-    own[0] = mma(z[0], ld8(p0), own[0]);
-    own[0] = mma(z[1], ld8(p0 + 32), own[0]);
-    st.update(ISV ? sQ : sD, ISV ? C::TQ::LD : C::TD::LD, z, t.E, t.eC, lane);
-    const auto out = chunk(O, so, n, wo);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      if (part)
-        la_putf(out, oo[i], own[i]);
-      else
-        la_put4(out, oo[i], own[i]);
-    }
-    __syncthreads();
-    if (wave == C::NW - 1 && lane < len) {
-      float x = 0.f;
-#pragma unroll
-      for (int w = 0; w < C::NWV; ++w) x += sB[w * CH + lane];
-      a.pb[((size_t)slice * a.geo.B * a.geo.T + row + lane) * H + h] = x * t.T[lane];
-      if (slice == 0) {
-        float rs = 0.f, cs = 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          rs += j <= g ? sRow[j * CH + lane] : 0.f;
-          cs += j >= g ? sCol[j * CH + lane] : 0.f;
+        if (i % 2 == 0) {
+          *reinterpret_cast<u4v*>(sS + sm) = er[i];
+          *reinterpret_cast<u4v*>(sS + sm + 1024) = er[i + 1];
+          la_wave_order();
         }
-        a.prc[(row + lane) * H + h] = rs - cs;
+        ev[i] = la_ld16(sS + sr + 1024 * (i % 2));
+#pragma unroll
+        for (int u = 0; u < 4; ++u) y += acc[0][i][u] * (float)ev[i][u] + acc[1][i][u] * (float)ev[i][4 + u];
+        if (i % 2) la_wave_order();
+      }
+      y += row_partner16(y, (lane & 16) != 0);
+      y += row_partner32(y, lane >= 32);
+      if (g == 0) sC[16 * wave + c] = y;
+    }
+    const __bf16* pf = sP + 256 * (g >> 1) + 16 * c + 8 * (g & 1);
+#pragma unroll
+    for (int q = PARTS - 1; q >= 0; --q)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (REV ? (kb == 1 || i < 2) : (kb == 0 || i >= 2)) {
+            const bf8 p = ld8(pf + q * kLaScores + 256 * la_ptile<REV>(i, 2 * kb));
+#pragma unroll
+            for (int k = 0; k < 2; ++k) acc[k][i] = mma(z[k][kb], p, acc[k][i]);
+          }
+    const auto bo = out.buf();
+    out.next(so);
+#pragma unroll
+    for (int i0 = 0; i0 < 4; i0 += 2) {
+      if constexpr (SUMS) {
+#pragma unroll
+        for (int i = i0; i < i0 + 2; ++i) {
+          float x = 0.f;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) x += acc[0][i][u] * (float)ev[i][u] + acc[1][i][u] * (float)ev[i][4 + u];
+          x += row_partner16(x, (lane & 16) != 0);
+          x += row_partner32(x, lane >= 32);
+          if (g == 0) sA[wave * CH + 16 * i + c] = x;
+          const float d = sDiag[16 * i + c];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            acc[0][i][u] += d * (float)zr[i][u];
+            acc[1][i][u] += d * (float)zr[i][4 + u];
+          }
+        }
+      }
+      if (part) {
+#pragma unroll
+        for (int i = i0; i < i0 + 2; ++i)
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4v, acc[k][i]), bo,
+                                                   (16 * i + c) * so + 4 * (32 * wave + 8 * g + 4 * k), 0, 0);
+      } else {
+#pragma unroll
+        for (int i = i0; i < i0 + 2; ++i) {
+          bf8 v;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) v[u] = (__bf16)acc[0][i][u], v[4 + u] = (__bf16)acc[1][i][u];
+          *reinterpret_cast<bf8*>(sS + sr + 1024 * (i - i0)) = v;
+        }
+        la_wave_order();
+#pragma unroll
+        for (int i = i0; i < i0 + 2; ++i)
+          __builtin_amdgcn_raw_buffer_store_b128(*reinterpret_cast<const u4v*>(sS + sm + 1024 * (i - i0)), bo, o0 + 16 * i * sz, 0, 0);
+        la_wave_order();
       }
     }
-    if (more) settle();
+    __builtin_amdgcn_sched_barrier(0);
+    st.template update<C::UPARTS>(sY, ax, z, REV ? t.E : t.T, lane);
+    if constexpr (ROLE == kLaDq) {
+      if ((n + 1) % kLaAnchor == 0 || !more)
+        st.template store<B, TR>(a.aS + ((size_t)unit * a.anchors + n / kLaAnchor) * (DK * DV), lane, wave);
+    }
+    if (part)  // behind the tiles' loads lie the output's stores, at an anchor more
+      la_landed<16>();
+    else
+      la_landed<4>();
   }
-  if constexpr (ISV) {
-    if (un.first && a.dS0) st.store(a.dS0 + ((size_t)un.seq * H + h) * (DK * DV), DV, b0, lane);
+  if constexpr (SUMS) {
+    __syncthreads();
+    if (wave == 0 && nc > 0) total(nc - 1);
+  }
+  if constexpr (ROLE == kLaO) {
+    if (un.last && a.ST) st.template store<B, TR>(a.ST + ((size_t)un.seq * H + h) * (DK * DV), lane, wave);
+  }
+  if constexpr (ROLE == kLaDv) {
+    if (un.first && a.dS0) st.template store<B, TR>(a.dS0 + ((size_t)un.seq * H + h) * (DK * DV), lane, wave);
   }
 }
 
-// The two roles meet at the same barriers: both run the same loop over the same chunks.
 template <int DK, int DV>
-__global__ __launch_bounds__((LaRevCfg<DK, DV>::NTHR)) void la_scan_dkv_kernel(LaScanArgs a) {
+__global__ __launch_bounds__(2 * DV, 2) void la_scan_fwd_kernel(LaScanArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
-  if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) < LaRevCfg<DK, DV>::NWV)
-    la_reverse<DK, DV, true>(a, smem);
+  la_scan<DK, DV, kLaO>(a, blockIdx.x, smem);
+}
+// The gradients side by side.
+template <int DK, int DV>
+__global__ __launch_bounds__(2 * (DK > DV ? DK : DV), 2) void la_scan_bwd_kernel(LaScanArgs a) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  int unit, role;
+  if (!la_slot<3>(blockIdx.x, a.segs.nslot * a.geo.H, unit, role)) return;
+  if (role == 0)
+    la_scan<DK, DV, kLaDq>(a, unit, smem);
+  else if (role == 1)
+    la_scan<DK, DV, kLaDk>(a, unit, smem);
   else
-    la_reverse<DK, DV, false>(a, smem);
+    la_scan<DK, DV, kLaDv>(a, unit, smem);
 }
 
 // ---- the decays' gradient --------------------------------------------------
-// dg_t = <S, dS> behind the last token of the stretch + sum over t' >= t of a + row - b - col,
-// in 64 bits; a stretch of up to kLaAnchor chunks a workgroup, a token a thread.
+// With a_t = q_t . dq_t and b_t = v_t . dv_t, dg_t is <S, dS> behind any later token plus the sum
+// of a - b from t up to it, taken in 64 bits.  Where t and that token are in one chunk, a and b
+// count without the diagonal's part, the same in both; chunks between count with what their a and
+// b have from the states alone, for pairs of tokens inside a chunk cancel, and what would be left
+// of them is rounding (1.8e-6 of dg at 4096 tokens of mean log-decay -0.13, against 0.8e-6).  A
+// stretch of up to kLaAnchor chunks from one <S, dS> a workgroup, a chunk a wave, a token a lane.
 template <int DK, int DV>
 __global__ __launch_bounds__(kLaAnchor * CH) void la_dg_kernel(LaScanArgs a) {
-  constexpr int NTHR = kLaAnchor * CH, NA = DK / 64, NB = LaRevCfg<DK, DV>::NS;
+  constexpr int NTHR = kLaAnchor * CH;
   __shared__ double part[NTHR / 64], phi[NTHR / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int H = a.geo.H, unit = blockIdx.x / a.anchors, k = blockIdx.x % a.anchors, h = unit % H;
@@ -975,14 +934,12 @@ __global__ __launch_bounds__(kLaAnchor * CH) void la_dg_kernel(LaScanArgs a) {
   const int t0 = k * NTHR, len = min(NTHR, un.len - t0);
   if (len <= 0) return;
   double x = 0.0;
-  const size_t row = un.row0 + t0 + tid, rows = (size_t)a.geo.B * a.geo.T;
-  if (tid < len) {
-    float pa = 0.f, pb = 0.f;
-#pragma unroll
-    for (int s = 0; s < NA; ++s) pa += a.pa[(s * rows + row) * H + h];
-#pragma unroll
-    for (int s = 0; s < NB; ++s) pb += a.pb[(s * rows + row) * H + h];
-    x = (double)pa + a.prc[row * H + h] - pb;
+  const size_t row = un.row0 + t0 + tid;
+  if (tid < len) x = (double)a.pa[row * H + h] - a.pb[row * H + h];
+  double y = 0.0;
+  if (wave * CH < len && lane < 16) {
+    const size_t i = ((size_t)unit * (a.segs.seg_tokens / CH) + k * kLaAnchor + wave) * 16 + lane;
+    y = (double)a.ca[i] - a.cb[i];
   }
   double f = 0.0;
   if (!(un.last && t0 + len == un.len && a.dST == nullptr)) {
@@ -994,12 +951,13 @@ __global__ __launch_bounds__(kLaAnchor * CH) void la_dg_kernel(LaScanArgs a) {
   }
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const double y = __shfl_down(x, o);
-    if (lane + o < 64) x += y;
+    const double z = __shfl_down(x, o);
+    if (lane + o < 64) x += z;
     f += __shfl_xor(f, o);
+    y += __shfl_xor(y, o);
   }
   if (lane == 0) {
-    part[wave] = x;
+    part[wave] = y;
     phi[wave] = f;
   }
   __syncthreads();
@@ -1067,12 +1025,9 @@ hipError_t la_launch(K kernel, unsigned grid, unsigned threads, size_t lds, cons
 
 template <int DK, int DV>
 hipError_t launch_la_segstate(const LaScanArgs& a, bool rev, hipStream_t st) {
-  const unsigned grid = la_grid<DV / 64>(a.segs.nslot * a.geo.H);
-  if (rev)
-    hipLaunchKernelGGL((la_segstate_kernel<DK, DV, true>), dim3(grid), dim3(512), 0, st, a);
-  else
-    hipLaunchKernelGGL((la_segstate_kernel<DK, DV, false>), dim3(grid), dim3(512), 0, st, a);
-  return hipGetLastError();
+  constexpr size_t lds = 2 * (la_bytes(DK) + la_bytes(DV) + sizeof(LaTab));
+  const auto kernel = rev ? la_segstate_kernel<DK, DV, true> : la_segstate_kernel<DK, DV, false>;
+  return la_launch(kernel, (unsigned)(a.segs.nslot * a.geo.H), 2 * DV, lds, a, st);
 }
 
 hipError_t launch_la_segcombine(const LaScanArgs& a, int size, bool rev, hipStream_t st) {
@@ -1083,17 +1038,15 @@ hipError_t launch_la_segcombine(const LaScanArgs& a, int size, bool rev, hipStre
 
 template <int DK, int DV>
 hipError_t launch_la_scan_fwd(const LaScanArgs& a, hipStream_t st) {
-  using C = LaFwdCfg<DK, DV, false>;
-  return la_launch(la_scan_fwd_kernel<DK, DV>, la_grid<C::NS>(a.segs.nslot * a.geo.H), C::NTHR, C::LDS, a, st);
+  return la_launch(la_scan_fwd_kernel<DK, DV>, (unsigned)(a.segs.nslot * a.geo.H), 2 * DV, LaCfg<DK, DV, kLaO>::LDS, a, st);
 }
 
 template <int DK, int DV>
 hipError_t launch_la_scan_bwd(const LaScanArgs& a, hipStream_t st) {
-  using CQ = LaFwdCfg<DK, DV, true>;
-  using CR = LaRevCfg<DK, DV>;
+  constexpr size_t lq = LaCfg<DK, DV, kLaDq>::LDS, lk = LaCfg<DK, DV, kLaDk>::LDS, lv = LaCfg<DK, DV, kLaDv>::LDS;
+  constexpr size_t lds = lq > lk ? (lq > lv ? lq : lv) : (lk > lv ? lk : lv);
   const int units = a.segs.nslot * a.geo.H;
-  hipError_t e = la_launch(la_scan_dq_kernel<DK, DV>, la_grid<CQ::NS>(units), CQ::NTHR, CQ::LDS, a, st);
-  if (e == hipSuccess) e = la_launch(la_scan_dkv_kernel<DK, DV>, la_grid<CR::NS>(units), CR::NTHR, CR::LDS, a, st);
+  hipError_t e = la_launch(la_scan_bwd_kernel<DK, DV>, la_grid<3>(units), 2 * (DK > DV ? DK : DV), lds, a, st);
   if (e == hipSuccess) {
     hipLaunchKernelGGL((la_dg_kernel<DK, DV>), dim3((unsigned)(units * a.anchors)), dim3(kLaAnchor * CH), 0, st, a);
     e = hipGetLastError();
