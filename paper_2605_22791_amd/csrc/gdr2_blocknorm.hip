@@ -80,6 +80,25 @@ __device__ __forceinline__ void norm_store(bf16_t* p, int D, int lane, const flo
   }
 }
 
+// A lane's part of a row on its way from memory: loaded a row ahead, in as few registers as it takes
+template <typename T, int LPR, bool VEC>
+struct NormRow {
+  float x[EPL];
+  __device__ __forceinline__ void load(const T* p, int D, int lane) { norm_load<LPR, VEC>(p, D, lane, x); }
+  __device__ __forceinline__ void get(float (&to)[EPL]) const {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) to[i] = x[i];
+  }
+};
+template <int LPR>
+struct NormRow<bf16_t, LPR, true> {
+  u4v x;
+  __device__ __forceinline__ void load(const bf16_t* p, int D, int lane) {
+    x = EPL * lane < D ? *reinterpret_cast<const u4v*>(p + EPL * lane) : u4v{0, 0, 0, 0};
+  }
+  __device__ __forceinline__ void get(float (&to)[EPL]) const { unpack8(__builtin_bit_cast(bf8, x), to); }
+};
+
 // Sums over a row's LPR lanes, every lane gets them.  Up to a wave: steps across
 // lanes; more: the waves' sums meet in LDS (slot: a different one of four at each of
 // a row's reductions, so that one barrier a reduction is enough).
@@ -195,36 +214,52 @@ __global__ __launch_bounds__(norm_threads<LPR>()) void norm_fwd_kernel(NormFwdAr
   }
 }
 
-template <typename T, typename TS, int LPR, bool VEC>
+// REST: there may be x, c or w_pre; without them a lane needs half the registers.
+template <typename T, typename TS, int LPR, bool VEC, bool REST>
 __global__ __launch_bounds__(norm_threads<LPR>()) void norm_bwd_kernel(NormBwdArgs<T, TS> a) {
   constexpr int TPB = norm_threads<LPR>(), RPB = TPB / LPR;
   __shared__ float red[norm_red<LPR>()];
   __shared__ float acc[RPB > 1 ? TPB * EPL : 1];
   const int lane = threadIdx.x % LPR, D = a.D;
+  const bool has_x = REST && a.x, has_c = REST && a.c, pre = REST && a.w_pre;
   float wp[EPL], c[EPL], wn[EPL], dwp[EPL], dc[EPL], dwn[EPL];
 #pragma unroll
   for (int i = 0; i < EPL; ++i) wp[i] = c[i] = 1.f, dwp[i] = dc[i] = dwn[i] = 0.f;
   if (a.w_post) norm_load<LPR, VEC>(a.w_post, D, lane, wp);
-  if (a.c) norm_load<LPR, VEC>(a.c, D, lane, c);
-  if (a.w_pre) norm_load<LPR, VEC>(a.w_pre, D, lane, wn);
+  if (has_c) norm_load<LPR, VEC>(a.c, D, lane, c);
+  if (pre) norm_load<LPR, VEC>(a.w_pre, D, lane, wn);
   using Acc = NormAcc<LPR>;
   const Acc inv_d = (Acc)1 / (Acc)D;
   int slot = 0;
-  for (int64_t base = (int64_t)blockIdx.x * RPB; base < a.rows; base += (int64_t)gridDim.x * RPB) {
+  NormRow<T, LPR, VEC> ny, nz, nt;
+  NormRow<TS, LPR, VEC> nx, ndh;
+  const auto fetch = [&](int64_t base) {
+    const int64_t row = base + threadIdx.x / LPR;
+    const size_t at = (size_t)(row < a.rows ? row : a.rows - 1) * D;
+    ny.load(a.y + at, D, lane);
+    if (a.z) nz.load(a.z + at, D, lane);
+    if (has_x) nx.load(a.x + at, D, lane);
+    if (a.dh) ndh.load(a.dh + at, D, lane);
+    if (pre) nt.load(a.dn + at, D, lane);
+  };
+  const int64_t step = (int64_t)gridDim.x * RPB;
+  fetch((int64_t)blockIdx.x * RPB);
+  for (int64_t base = (int64_t)blockIdx.x * RPB; base < a.rows; base += step) {
     const int64_t row = base + threadIdx.x / LPR;
     const bool on = row < a.rows;
     const size_t at = (size_t)(on ? row : a.rows - 1) * D;
     float y[EPL], z[EPL], h[EPL], dh[EPL], t[EPL];
-    norm_load<LPR, VEC>(a.y + at, D, lane, y);
-    if (a.z) norm_load<LPR, VEC>(a.z + at, D, lane, z);
-    if (a.x) norm_load<LPR, VEC>(a.x + at, D, lane, h);
+    ny.get(y);
+    if (a.z) nz.get(z);
+    if (has_x) nx.get(h);
     if (a.dh) {
-      norm_load<LPR, VEC>(a.dh + at, D, lane, dh);
+      ndh.get(dh);
     } else {
 #pragma unroll
       for (int i = 0; i < EPL; ++i) dh[i] = 0.f;
     }
-    if (a.w_pre) norm_load<LPR, VEC>(a.dn + at, D, lane, t);
+    if (pre) nt.get(t);
+    if (base + step < a.rows) fetch(base + step);
     Acc rya = 1;
     if (a.w_post) {
       Acc s[1] = {0};
@@ -240,12 +275,12 @@ __global__ __launch_bounds__(norm_threads<LPR>()) void norm_bwd_kernel(NormBwdAr
       for (int i = 0; i < EPL; ++i) sg[i] = 1.f / (1.f + expf(-z[i]));
     }
     // full gradient at h, in dh
-    if (a.w_pre) {
+    if (pre) {
       Acc s[2] = {0, 0};
 #pragma unroll
       for (int i = 0; i < EPL; ++i) {
         const float v = y[i] * ry * wp[i] * (a.z ? z[i] * sg[i] : 1.f) * c[i];
-        h[i] = a.x ? h[i] + v : v;
+        h[i] = has_x ? h[i] + v : v;
         s[0] += (Acc)h[i] * h[i];
         s[1] += (Acc)(t[i] * wn[i]) * h[i];
       }
@@ -257,12 +292,12 @@ __global__ __launch_bounds__(norm_threads<LPR>()) void norm_bwd_kernel(NormBwdAr
         dh[i] += (float)(rh * (t[i] * wn[i] - h[i] * m));
       }
     }
-    if (a.dx && on) norm_store<LPR, VEC>(a.dx + at, D, lane, dh);
+    if (has_x && a.dx && on) norm_store<LPR, VEC>(a.dx + at, D, lane, dh);
     float dz[EPL];
 #pragma unroll
     for (int i = 0; i < EPL; ++i) {
       const float u = y[i] * ry * wp[i], s = a.z ? z[i] * sg[i] : 1.f;
-      if (on) dc[i] += dh[i] * u * s;
+      if (has_c && on) dc[i] += dh[i] * u * s;
       const float da = dh[i] * c[i];
       if (a.z) dz[i] = da * u * sg[i] * (1.f + z[i] * (1.f - sg[i]));
       dh[i] = da * s;
@@ -299,25 +334,29 @@ __global__ __launch_bounds__(norm_threads<LPR>()) void norm_bwd_kernel(NormBwdAr
     }
   };
   if (a.w_post) leave(dwp, 0);
-  if (a.c) leave(dc, 1);
-  if (a.w_pre) leave(dwn, 2);
+  if (has_c) leave(dc, 1);
+  if (pre) leave(dwn, 2);
 }
 
-// Columns' sums over the workgroups: 16 columns a workgroup, 16 threads each
-__global__ __launch_bounds__(256) void norm_sum_kernel(NormSumArgs a) {
-  __shared__ float sum[16][17];
+// Columns' sums over the workgroups: 16 columns a workgroup, 64 threads each, so that a column's
+// loads are in flight together (16 threads each took 20 us for 1024 parts of 128 to 2048 columns)
+__global__ __launch_bounds__(1024) void norm_sum_kernel(NormSumArgs a) {
+  __shared__ float sum[64][17];
   const int j = threadIdx.x % 16, g = threadIdx.x / 16, col = blockIdx.x * 16 + j, k = blockIdx.y;
   float* out = a.out[k];
   if (out == nullptr) return;
   float x = 0.f;
-  if (col < a.D)
-    for (int b = g; b < a.blocks; b += 16) x += a.part[((size_t)k * a.blocks + b) * a.D + col];
+  if (col < a.D) {
+    const float* p = a.part + (size_t)k * a.blocks * a.D + col;
+#pragma unroll 16
+    for (int b = g; b < a.blocks; b += 64) x += p[(size_t)b * a.D];
+  }
   sum[g][j] = x;
   __syncthreads();
   if (g == 0 && col < a.D) {
     float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s += sum[i][j];
+    for (int i = 0; i < 64; ++i) s += sum[i][j];
     out[col] = s;
   }
 }
@@ -356,10 +395,12 @@ hipError_t norm_dispatch(int D, F&& f) {
 
 }  // namespace
 
-int norm_bwd_blocks(int64_t rows, int D) {
+// Workgroups of a backward call, as many as are resident together: four waves a SIMD of the form
+// without x, c and w_pre, two of the other (at 1024 for both, rows of 2048 took 382 us for 340)
+int norm_bwd_blocks(int64_t rows, int D, bool rest) {
   const int rpb = norm_rows_per_block(D);
-  const int64_t n = (rows + rpb - 1) / rpb;
-  return (int)(n < 1024 ? n : 1024);
+  const int64_t n = (rows + rpb - 1) / rpb, most = rest ? 512 : 1024;
+  return (int)(n < most ? n : most);
 }
 
 template <typename T, typename TS>
@@ -377,14 +418,15 @@ template <typename T, typename TS>
 hipError_t launch_norm_bwd(const NormBwdArgs<T, TS>& a, hipStream_t st) {
   return norm_dispatch(a.D, [&](auto lpr, auto vec) {
     constexpr int LPR = decltype(lpr)::value;
-    hipLaunchKernelGGL((norm_bwd_kernel<T, TS, LPR, decltype(vec)::value>), dim3((unsigned)a.blocks),
-                       dim3(norm_threads<LPR>()), 0, st, a);
+    const auto kernel = a.x || a.c || a.w_pre ? norm_bwd_kernel<T, TS, LPR, decltype(vec)::value, true>
+                                              : norm_bwd_kernel<T, TS, LPR, decltype(vec)::value, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)a.blocks), dim3(norm_threads<LPR>()), 0, st, a);
     return hipGetLastError();
   });
 }
 
 hipError_t launch_norm_sum(const NormSumArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL(norm_sum_kernel, dim3((unsigned)((a.D + 15) / 16), 3), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(norm_sum_kernel, dim3((unsigned)((a.D + 15) / 16), 3), dim3(1024), 0, st, a);
   return hipGetLastError();
 }
 

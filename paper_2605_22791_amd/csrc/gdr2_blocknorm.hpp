@@ -39,7 +39,7 @@ struct NormSumArgs {
 };
 
 // workgroups of the backward: its rows' partial sums
-int norm_bwd_blocks(int64_t rows, int D);
+int norm_bwd_blocks(int64_t rows, int D, bool rest);
 
 template <typename T, typename TS>
 hipError_t launch_norm_fwd(const NormFwdArgs<T, TS>& a, hipStream_t st);

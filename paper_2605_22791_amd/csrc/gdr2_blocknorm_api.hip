@@ -25,7 +25,7 @@ gdr2_status norm_check(const gdr2_blocknorm* p) {
   return GDR2_OK;
 }
 
-size_t norm_ws(const gdr2_blocknorm* p) { return round_up((size_t)3 * norm_bwd_blocks(p->rows, p->D) * p->D * 4); }
+size_t norm_ws(const gdr2_blocknorm* p) { return round_up((size_t)3 * norm_bwd_blocks(p->rows, p->D, false) * p->D * 4); }
 
 // f(T{}, TS{}): the types of y and of h
 template <class F>
@@ -77,7 +77,7 @@ gdr2_status gdr2_blocknorm_bwd(const gdr2_blocknorm* p, const void* y, const flo
   const bool sums = w_post != nullptr || c != nullptr || w_pre != nullptr;
   if (sums && p->rows > 0 && ws == nullptr) return GDR2_EINVAL;
   if (sums && ws_bytes < norm_ws(p)) return GDR2_EWORKSPACE;
-  const int blocks = norm_bwd_blocks(p->rows, p->D);
+  const int blocks = norm_bwd_blocks(p->rows, p->D, x != nullptr || c != nullptr || w_pre != nullptr);
   hipError_t e = hipSuccess;
   if (p->rows > 0)
     e = norm_types(p, x != nullptr, [&](auto t, auto ts) {
