@@ -20,8 +20,8 @@
  *     g, dg                 (B, T, Hv) or (Hv)            fp32
  *     S0, S_T, S, dS_T, dS0 (B, Hv, Dk, Dv), packed (n_seqs, Hv, Dk, Dv)   fp32
  * A token has at most 2^22 values over all heads in a chunk call (Hv * max(Dk, Dv),
- * else GDR2_EUNSUPPORTED).  Pointers are 16-byte aligned (cu_seqlens: 4-byte).  Outputs are overwritten.  An
- * empty sequence of a packed batch passes S0 to S_T and dS_T to dS0.
+ * else GDR2_EUNSUPPORTED).  Pointers are 16-byte aligned (cu_seqlens: 4-byte).  Outputs
+ * are overwritten.  An empty sequence of a packed batch passes S0 to S_T and dS_T to dS0.
  *
  * A non-finite value in a token's q, k, v or dout reaches the outputs of its own
  * 64-token chunk on both sides of the token, and what follows from the state.

@@ -4,6 +4,8 @@
 
 #include "../../include/gdr2_linattn.h"
 
+#include <algorithm>
+
 #include "gdr2_host.hpp"
 #include "gdr2_linattn.hpp"
 
@@ -29,16 +31,20 @@ struct LaLayout {
   bool multi;  // sequences of more than one segment
 };
 
-// Tokens of a segment.  A workgroup scans one head's segment; whole sequences while there are
-// enough of those to give every CU two, else cut until there are, down to two chunks.  A packed
-// batch counts as one sequence: its lengths are on the device.
+// Tokens of a segment.  A workgroup scans one head's segment, two are on a CU at a time: sequences
+// are cut into as many as fill the 256 CUs once.  (Twice as many, in two rounds, took 89 us where
+// one round took 81, nine packed prompts of 8192 tokens in all, 16 value heads: each segment
+// costs its state's way to memory and back.)  A packed batch counts as one sequence of its total
+// length, beside a slot for the end of each, for its lengths are on the device.  Cutting takes two
+// more launches: up to three chunks (T 192, 16 heads: 15.2 us whole, 17.1 cut) are left whole.
 int la_seg_tokens(const gdr2_problem* p, int nseq) {
   const int NT = chunks_per_seq(p);
-  const long long base = (long long)(nseq > 0 ? 1 : p->B) * value_view(p).H;
-  int chunks = NT;
-  while (base * ((NT + chunks - 1) / chunks) < 512 && chunks > 2) chunks = (chunks + 1) / 2;
+  const long long H = value_view(p).H, base = (nseq > 0 ? 1 : p->B) * H;
+  const long long most = nseq > 0 ? std::max(512 - nseq * H, 256LL) : 512;
+  const int nseg = (int)std::max(1LL, std::min(most / base, (long long)NT));
+  int chunks = NT <= 3 ? NT : (NT + nseg - 1) / nseg;
   // a segment's rows, the widest in fp32, are one buffer of at most 2^31 bytes
-  const long long row = 4LL * value_view(p).H * (p->Dk > p->Dv ? p->Dk : p->Dv);
+  const long long row = 4LL * H * std::max(p->Dk, p->Dv);
   while (chunks > 1 && chunks * CH * row > (1LL << 31)) chunks = (chunks + 1) / 2;
   return chunks * CH;
 }
@@ -257,14 +263,16 @@ hipError_t la_dispatch(const gdr2_problem* p, F&& f) {
   return p->dtype == GDR2_BF16 ? dims(bf16_t{}) : dims(0.f);
 }
 
+// a chunk's rows are reached by 32-bit byte offsets (fp32 parts of grouped heads among them)
+bool la_wide(const gdr2_problem* p) { return (double)value_view(p).H * std::max(p->Dk, p->Dv) > kMaxRow; }
+
 // n_seqs as the calls take it: 0 for a fixed-length batch
 gdr2_status la_check(const gdr2_problem* p, int decay, const int32_t* cu, int n_seqs, bool chunked) {
   if (n_seqs < 0) return GDR2_EINVAL;
   const gdr2_status s = check_problem(p, chunked, n_seqs);
   if (s != GDR2_OK) return s;
   if (!decay_ok(decay)) return GDR2_EINVAL;
-  // a chunk's rows are reached by 32-bit byte offsets (fp32 parts of grouped heads among them)
-  if (chunked && (double)value_view(p).H * (p->Dk > p->Dv ? p->Dk : p->Dv) > kMaxRow) return GDR2_EUNSUPPORTED;
+  if (chunked && la_wide(p)) return GDR2_EUNSUPPORTED;
   if (n_seqs > 0 && (cu == nullptr || (reinterpret_cast<uintptr_t>(cu) & 3u) != 0)) return GDR2_EINVAL;
   return GDR2_OK;
 }
@@ -280,6 +288,7 @@ gdr2_status gdr2_linattn_workspace_bytes(const gdr2_problem* p, int32_t n_seqs, 
   if (bytes == nullptr || n_seqs < 0) return GDR2_EINVAL;
   const gdr2_status s = check_problem(p, true, n_seqs);
   if (s != GDR2_OK) return s;
+  if (la_wide(p)) return GDR2_EUNSUPPORTED;
   *bytes = la_layout(p, for_backward != 0, n_seqs).total;
   return GDR2_OK;
 }

@@ -40,6 +40,8 @@ namespace gdr2 {
 
 namespace {
 
+enum LaRole : int { kLaO, kLaDq, kLaDv, kLaDk };
+
 struct LaUnit {
   size_t row0;
   int len, seq, slot;
@@ -70,16 +72,21 @@ __device__ __forceinline__ bool la_unit(const LaSegs& s, int T, int slot, LaUnit
   return true;
 }
 
-// Workgroup b of a grid of (unit, role): the NR roles of a unit run on one XCD (blocks go to the
-// eight XCDs in turn) and share its L2; unit < n.
-template <int NR>
+// Workgroup b of the gradients' grid: first dq and dv, the longer ones, of eight units after each
+// other, then dk.  Blocks go to the eight XCDs in turn, so a unit's run on one and share its L2.
+// (All three of a unit together took 543 us for 521 at 8 x 4096 tokens, 16 heads: a tail of long ones.)
 __device__ __forceinline__ bool la_slot(int b, int n, int& unit, int& role) {
-  unit = b / (8 * NR) * 8 + b % 8;
-  role = b / 8 % NR;
+  const int n8 = (n + 7) / 8 * 8;
+  if (b < 2 * n8) {
+    unit = b / 16 * 8 + b % 8;
+    role = b / 8 % 2 ? kLaDv : kLaDq;
+  } else {
+    unit = b - 2 * n8;
+    role = kLaDk;
+  }
   return unit < n;
 }
-template <int NR>
-unsigned la_grid(int n) { return (unsigned)((n + 7) / 8 * 8) * NR; }
+unsigned la_grid(int n) { return (unsigned)((n + 7) / 8 * 8) * 3; }
 
 // ---- decays of a chunk -----------------------------------------------------
 // Sums are taken within the blocks of 16 rows in 64 bits, p_r up to and including r, so that
@@ -553,12 +560,11 @@ __global__ __launch_bounds__(2 * DV, 2) void la_segstate_kernel(LaScanArgs a) {
   st.zero();
   float graw = 0.f;
   if (nc > 0) {
-    if (wave == TW) {
-      graw = decay(0);
-      gs += (double)la_tables(graw, rows(0), tab[0], lane, scale);
-      if (nc > 1) graw = decay(1);
-    }
+    // all that comes from memory on its way at once
+    const float g0 = wave == TW ? decay(0) : 0.f;
+    if (wave == TW && nc > 1) graw = decay(1);
     fetch(0);
+    if (wave == TW) gs += (double)la_tables(g0, rows(0), tab[0], lane, scale);
   }
   for (int n = 0; n < nc; ++n) {
     la_landed<0>();
@@ -625,7 +631,6 @@ __global__ __launch_bounds__(256) void la_segcombine_kernel(LaScanArgs a, int si
 }
 
 // ---- the scans ---------------------------------------------------------------
-enum LaRole : int { kLaO, kLaDq, kLaDv, kLaDk };
 
 template <int DK, int DV, int ROLE>
 struct LaCfg {
@@ -677,6 +682,26 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
   const LaDecays decays(a.geo, un.row0, h, lane);
   const auto decay = [&](int n) { return decays.load(at(n), rows(n)); };
 
+  const unsigned lds = la_lds(smem);
+  const LaLoad<A, NW> lx(sx, lane, wave);
+  const LaLoad<B, NW> lz(sz, lane, wave);
+  const LaAt ax(lane, wave);
+  // Rows of E and of the output in memory are four lanes' sixteen bytes (a quarter of the address
+  // cycles of a row a lane); they pass through the wave's own two kilobytes, 32 rows at a time.
+  const unsigned o0 = (lane >> 2) * sz + 64 * wave + 16 * (lane & 3);
+  unsigned char* sS = smem + C::OFF_S + 2048 * wave;
+  const int sm = 64 * (lane >> 2) + (((lane & 3) ^ (-(lane >> 4) & 3)) << 4);  // as in memory: row lane >> 2, piece lane & 3
+  const int sr = 64 * c + ((g ^ (-(c >> 2) & 3)) << 4);                        // as the products have it: row c, piece g
+  // all that comes from memory on its way at once
+  float g0 = 0.f, graw = 0.f;
+  if (nc > 0) {
+    if (wave == TW) {
+      g0 = decay(0);
+      if (nc > 1) graw = decay(1);
+    }
+    lx.load(X, sx, lds, wave);
+    lz.load(Z, sz, lds + C::OFF_Z, wave);
+  }
   LaState<A> st;
   {
     const float* given = REV ? a.dST : a.S0;
@@ -688,22 +713,8 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
     else
       st.template load<B, TR>(init, lane, wave);
   }
-  const unsigned lds = la_lds(smem);
-  const LaLoad<A, NW> lx(sx, lane, wave);
-  const LaLoad<B, NW> lz(sz, lane, wave);
-  const LaAt ax(lane, wave);
-  // Rows of E and of the output in memory are four lanes' sixteen bytes (a quarter of the address
-  // cycles of a row a lane); they pass through the wave's own two kilobytes, 32 rows at a time.
-  const unsigned o0 = (lane >> 2) * sz + 64 * wave + 16 * (lane & 3);
-  unsigned char* sS = smem + C::OFF_S + 2048 * wave;
-  const int sm = 64 * (lane >> 2) + (((lane & 3) ^ (-(lane >> 4) & 3)) << 4);  // as in memory: row lane >> 2, piece lane & 3
-  const int sr = 64 * c + ((g ^ (-(c >> 2) & 3)) << 4);                        // as the products have it: row c, piece g
-  float graw = 0.f;
   if (nc > 0) {
-    if (wave == TW) {
-      la_tables(decay(0), rows(0), tab[0], lane, scale);
-      if (nc > 1) graw = decay(1);
-    }
+    if (wave == TW) la_tables(g0, rows(0), tab[0], lane, scale);
     if (wave == 0) {  // the tiles past the diagonal
 #pragma unroll
       for (int k = 0; k < PARTS; ++k) {
@@ -711,8 +722,6 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
         *reinterpret_cast<bf4*>(sP + k * kLaScores + (REV ? la_ptile<REV>(3, 2) : la_ptile<REV>(2, 3)) * 256 + 4 * lane) = bf4{};
       }
     }
-    lx.load(X, sx, lds, wave);
-    lz.load(Z, sz, lds + C::OFF_Z, wave);
     la_landed<0>();
   }
   // chunk n's terms over the waves, a barrier after they were left
@@ -907,10 +916,10 @@ template <int DK, int DV>
 __global__ __launch_bounds__(2 * (DK > DV ? DK : DV), 2) void la_scan_bwd_kernel(LaScanArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
   int unit, role;
-  if (!la_slot<3>(blockIdx.x, a.segs.nslot * a.geo.H, unit, role)) return;
-  if (role == 0)
+  if (!la_slot(blockIdx.x, a.segs.nslot * a.geo.H, unit, role)) return;
+  if (role == kLaDq)
     la_scan<DK, DV, kLaDq>(a, unit, smem);
-  else if (role == 1)
+  else if (role == kLaDk)
     la_scan<DK, DV, kLaDk>(a, unit, smem);
   else
     la_scan<DK, DV, kLaDv>(a, unit, smem);
@@ -1046,7 +1055,7 @@ hipError_t launch_la_scan_bwd(const LaScanArgs& a, hipStream_t st) {
   constexpr size_t lq = LaCfg<DK, DV, kLaDq>::LDS, lk = LaCfg<DK, DV, kLaDk>::LDS, lv = LaCfg<DK, DV, kLaDv>::LDS;
   constexpr size_t lds = lq > lk ? (lq > lv ? lq : lv) : (lk > lv ? lk : lv);
   const int units = a.segs.nslot * a.geo.H;
-  hipError_t e = la_launch(la_scan_bwd_kernel<DK, DV>, la_grid<3>(units), 2 * (DK > DV ? DK : DV), lds, a, st);
+  hipError_t e = la_launch(la_scan_bwd_kernel<DK, DV>, la_grid(units), 2 * (DK > DV ? DK : DV), lds, a, st);
   if (e == hipSuccess) {
     hipLaunchKernelGGL((la_dg_kernel<DK, DV>), dim3((unsigned)(units * a.anchors)), dim3(kLaAnchor * CH), 0, st, a);
     e = hipGetLastError();

@@ -145,3 +145,14 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
             call()
     with pytest.raises(TypeError):
         g2.gdr2_blocknorm_fwd(torch.zeros((4, 8), dtype=torch.float16))
+
+
+def test_a_token_of_a_chunk_call_has_at_most_two_to_the_22_values():
+    wide = dict(H=1 << 15, Hv=(1 << 15) + (1 << 15), T=64, B=1)  # 2^16 value heads of 128: 2^23 values
+    for which in ("fwd", "bwd"):
+        assert _la(which, _prob(**wide)) == g2.GDR2_EUNSUPPORTED
+    n = ctypes.c_size_t(0)
+    assert g2.lib().gdr2_linattn_workspace_bytes(ctypes.byref(_prob(**wide)), 0, 1, ctypes.byref(n)) == g2.GDR2_EUNSUPPORTED
+    # at the bound itself the call is counted
+    assert g2.lib().gdr2_linattn_workspace_bytes(ctypes.byref(_prob(H=1 << 15, T=64, B=1)), 0, 1, ctypes.byref(n)) == g2.GDR2_OK
+    assert n.value > 0
