@@ -99,11 +99,28 @@ struct alignas(16) LaTab {
   float eC, pad[3];
 };
 
+// Row 16 i + c's sum of x[i] over g, in lane 16 i + c (each swap serves two values)
+__device__ __forceinline__ float la_sum4(const float (&x)[4]) {
+  const auto halves = [](float a, float b) {  // a's sum over halves in the lower lanes, b's in the upper
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  };
+  const float a = halves(x[0], x[2]), b = halves(x[1], x[3]);
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 template <int CTRL>
 __device__ __forceinline__ double la_dpp(double x) {
   const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(x), CTRL, 0xF, 0xF, true);
   const int hi = __builtin_amdgcn_update_dpp(0, __double2hiint(x), CTRL, 0xF, 0xF, true);
   return __hiloint2double(hi, lo);
+}
+// x as if new: lanes' conditions formed from it stay inside the loop they are in, where kept over
+// it their masks would take the scalar registers and spill
+__device__ __forceinline__ int la_new(int x) {
+  asm("" : "+v"(x));
+  return x;
 }
 __device__ __forceinline__ float la_lanef(float x, int lane) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane));
@@ -113,6 +130,7 @@ __device__ __forceinline__ float la_ex(float x) { return ex2(x * kLog2e); }
 // One wave, a row a lane: g the row's raw log-decay; rows past the chunk's end do not decay.
 // Returns the row's log-decay.
 __device__ __forceinline__ float la_tables(float g, int rows, LaTab& t, int lane, float scale) {
+  lane = la_new(lane);
   const float g0 = lane < rows ? (g < kLaForget ? kLaForget : g) : 0.f;
   double p = (double)g0 * 1.4426950408889634;
   p += la_dpp<0x111>(p);  // row_shr 1, 2, 4, 8
@@ -233,9 +251,12 @@ struct LaLoad {
   template <bool REV>
   __device__ __forceinline__ void load(const LaRows<REV>& r, unsigned stride, unsigned lds, int wave) const {
     const u4v buf = {(unsigned)(uintptr_t)r.p, (unsigned)((uintptr_t)r.p >> 32) & 0xffffu, r.left, 0x00020000u};
+    // formed anew at each call: kept over a loop, the many scalar values would spill into vector lanes
+    unsigned to = lds + wave * (NP * 1024), step = 8 * stride;
+    asm("" : "+s"(to), "+s"(step));
 #pragma unroll
     for (int m = 0; m < NP; ++m) {
-      const unsigned from = (off ^ (m & 1 ? 0x30 : 0)) + 8 * m * stride, at = lds + (wave * NP + m) * 1024;  // f(8) = 3
+      const unsigned from = (off ^ (m & 1 ? 0x30 : 0)) + m * step, at = to + m * 1024;  // f(8) = 3
       asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(from), "s"(buf) : "memory");
     }
   }
@@ -395,12 +416,13 @@ struct LaState {
       for (int k = 0; k < 2; ++k) {
         float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float z = s[k][2 * p + e / 4][e % 4];
-          const float y = z * eC;
-          asm("" : "+v"(z) : "v"(y));  // the decayed value lies elsewhere: the split takes this one's place
-          s[k][2 * p + e / 4][e % 4] = y;
-          x[e] = z;
+        for (int e = 0; e < 2; ++e) {
+          f4 z = s[k][2 * p + e];
+          const f4 y = z * eC;
+          asm("" : "+v"(z) : "v"(y));  // the decayed values lie elsewhere: the split takes these ones' place
+          s[k][2 * p + e] = y;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) x[4 * e + u] = z[u];
         }
         const LaFr<PARTS> f = la_split8<PARTS>(x);
 #pragma unroll
@@ -474,6 +496,7 @@ __device__ __forceinline__ f4 la_score(const unsigned char* Am, const unsigned c
 // r (s = s0 + c).  i, j: the blocks of r and s; on the diagonal itself D is 1.
 template <bool ROWS_S>
 __device__ __forceinline__ f4 la_decay_tile(const LaTab& t, int i, int j, int lane, float scale) {
+  lane = la_new(lane);
   const int g = lane >> 4, c = lane & 15;
   f4 d;
   if (i != j) {
@@ -782,12 +805,10 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
         if constexpr (SUMS) {
           // the diagonal cancels between a and b: it is kept out of both and added to the output by itself
           if (i == j) {
+            const int u0 = la_new(c - 4 * g);
+            if ((unsigned)u0 < 4u) sDiag[16 * i + c] = u0 < 2 ? (u0 == 0 ? x[0] : x[1]) : (u0 == 2 ? x[2] : x[3]);
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-              if (4 * g + u == c) {
-                sDiag[16 * i + c] = x[u];
-                x[u] = 0.f;
-              }
+            for (int u = 0; u < 4; ++u) x[u] = u == u0 ? 0.f : x[u];
           }
         }
         la_split4<PARTS>(sP + la_ptile<REV>(io, jz) * 256 + 16 * c + 4 * g, kLaScores, x);
@@ -840,6 +861,7 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
 #pragma unroll
             for (int k = 0; k < 2; ++k) acc[k][i] = mma(z[k][kb], p, acc[k][i]);
           }
+    float sum[SUMS ? 4 : 1];
     const auto bo = out.buf();
     out.next(so);
 #pragma unroll
@@ -850,9 +872,7 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
           float x = 0.f;
 #pragma unroll
           for (int u = 0; u < 4; ++u) x += acc[0][i][u] * (float)ev[i][u] + acc[1][i][u] * (float)ev[i][4 + u];
-          x += row_partner16(x, (lane & 16) != 0);
-          x += row_partner32(x, lane >= 32);
-          if (g == 0) sA[wave * CH + 16 * i + c] = x;
+          sum[i] = x;
           const float d = sDiag[16 * i + c];
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
@@ -883,6 +903,7 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
         la_wave_order();
       }
     }
+    if constexpr (SUMS) sA[wave * CH + lane] = la_sum4(sum);
     __builtin_amdgcn_sched_barrier(0);
     st.template update<C::UPARTS>(sY, ax, z, REV ? t.E : t.T, lane);
     if constexpr (ROLE == kLaDq) {
