@@ -17,16 +17,15 @@ namespace gdr2 {
 namespace {
 
 constexpr int kThr = 256;
+// The passes over chunks: as many waves as their tiles share out to, for one workgroup (the tiles
+// take up to 152 KB of LDS) has a CU to itself and only its own waves to hide what they wait for.
+// At 2 x 1000 tokens, 8 heads of 128, with four waves each: states 15.8 us, outputs 30, gradients 85;
+// with eight and sixteen 12.5, 18.6, 49.
+constexpr int kThrState = 512, kThrRows = 1024;
 
-__device__ __forceinline__ float la_in(const float* p) { return *p; }
 __device__ __forceinline__ void la_load4(const float* p, float (&x)[4]) {
   const float4 t = ld4(p);
   x[0] = t.x, x[1] = t.y, x[2] = t.z, x[3] = t.w;
-}
-__device__ __forceinline__ void la_load4(const bf16_t* p, float (&x)[4]) {
-  const uint2 t = *reinterpret_cast<const uint2*>(p);
-  x[0] = __uint_as_float(t.x << 16), x[1] = __uint_as_float(t.x & 0xffff0000u);
-  x[2] = __uint_as_float(t.y << 16), x[3] = __uint_as_float(t.y & 0xffff0000u);
 }
 __device__ __forceinline__ void la_put(float* p, float x) { *p = x; }
 __device__ __forceinline__ void la_put(bf16_t* p, float x) {
@@ -56,9 +55,9 @@ __device__ __forceinline__ void la_sums(const LaGeo& a, const ChunkPos& p, int h
 __device__ __forceinline__ float la_exp(double x) { return expf((float)x); }
 
 // 64 x D tile of one head into LDS as fp32 (row stride D + 4), rows >= len zero.
-template <int D, typename TIn>
+template <int D, int NTHR, typename TIn>
 __device__ __forceinline__ void la_tile(const TIn* src, size_t stride, int len, float* dst, int tid) {
-  for (int e = tid; e < CH * D / 4; e += kThr) {
+  for (int e = tid; e < CH * D / 4; e += NTHR) {
     const int r = e / (D / 4), c = (e % (D / 4)) * 4;
     float x[4] = {0.f, 0.f, 0.f, 0.f};
     if (r < len) la_load4(src + r * stride + c, x);
@@ -143,7 +142,7 @@ __device__ __forceinline__ f4 la_cols_tile(const float* P, const float* Z, int j
 
 // ---- every chunk's contribution to the state -------------------------------
 template <int DK, int DV, typename TIn, bool REV>
-__global__ __launch_bounds__(kThr) void la_state_kernel(LaStateArgs<TIn> a) {
+__global__ __launch_bounds__(kThrState) void la_state_kernel(LaStateArgs<TIn> a) {
   __shared__ double sG[CH + 1];
   __shared__ float sW[CH];
   extern __shared__ __align__(16) float smem[];
@@ -153,8 +152,8 @@ __global__ __launch_bounds__(kThr) void la_state_kernel(LaStateArgs<TIn> a) {
   ChunkPos p;
   if (!la_chunk(a.geo, blockIdx.x, h, p)) return;
   const int HK = a.geo.H / a.geo.G, hk = h / a.geo.G;
-  la_tile<DK>(a.x + (p.row0 * HK + hk) * DK, (size_t)HK * DK, p.len, sX, tid);
-  la_tile<DV>(a.z + (p.row0 * a.geo.H + h) * DV, (size_t)a.geo.H * DV, p.len, sZ, tid);
+  la_tile<DK, kThrState>(a.x + (p.row0 * HK + hk) * DK, (size_t)HK * DK, p.len, sX, tid);
+  la_tile<DV, kThrState>(a.z + (p.row0 * a.geo.H + h) * DV, (size_t)a.geo.H * DV, p.len, sZ, tid);
   la_sums(a.geo, p, h, sG, tid);
   __syncthreads();
   if (tid < CH) sW[tid] = REV ? a.geo.scale * la_exp(sG[tid + 1]) : la_exp(sG[CH] - sG[tid + 1]);
@@ -163,7 +162,7 @@ __global__ __launch_bounds__(kThr) void la_state_kernel(LaStateArgs<TIn> a) {
   constexpr int NV = DV / 16;
   const int g = lane >> 4, l = lane & 15;
   float* N = a.N + p.ch * (size_t)(DK * DV);
-  for (int cb = wave; cb < DK / 16; cb += kThr / 64) {
+  for (int cb = wave; cb < DK / 16; cb += kThrState / 64) {
     f4 acc[NV];
 #pragma unroll
     for (int t = 0; t < NV; ++t) acc[t] = f4{0.f, 0.f, 0.f, 0.f};
@@ -215,22 +214,23 @@ __global__ __launch_bounds__(kThr) void la_combine_kernel(LaCombineArgs a) {
 }
 
 // ---- outputs ---------------------------------------------------------------
+// wave 4 m + i: rows 16 i .., every fourth block of columns from m on
 template <int DK, int DV, typename TIn>
-__global__ __launch_bounds__(kThr) void la_fwd_kernel(LaFwdArgs<TIn> a) {
+__global__ __launch_bounds__(kThrRows) void la_fwd_kernel(LaFwdArgs<TIn> a) {
   __shared__ double sG[CH + 1];
   extern __shared__ __align__(16) float smem[];
   float *sQ = smem, *sK = sQ + CH * (DK + 4), *sV = sK + CH * (DK + 4), *sP = sV + CH * (DV + 4);
-  const int tid = threadIdx.x, lane = tid & 63, i = tid >> 6, g = lane >> 4, l = lane & 15;
+  const int tid = threadIdx.x, lane = tid & 63, i = (tid >> 6) & 3, m = tid >> 8, g = lane >> 4, l = lane & 15;
   int h;
   ChunkPos p;
   if (!la_chunk(a.geo, blockIdx.x, h, p)) return;
   const int H = a.geo.H, HK = H / a.geo.G, hk = h / a.geo.G;
-  la_tile<DK>(a.q + (p.row0 * HK + hk) * DK, (size_t)HK * DK, p.len, sQ, tid);
-  la_tile<DK>(a.k + (p.row0 * HK + hk) * DK, (size_t)HK * DK, p.len, sK, tid);
-  la_tile<DV>(a.v + (p.row0 * H + h) * DV, (size_t)H * DV, p.len, sV, tid);
+  la_tile<DK, kThrRows>(a.q + (p.row0 * HK + hk) * DK, (size_t)HK * DK, p.len, sQ, tid);
+  la_tile<DK, kThrRows>(a.k + (p.row0 * HK + hk) * DK, (size_t)HK * DK, p.len, sK, tid);
+  la_tile<DV, kThrRows>(a.v + (p.row0 * H + h) * DV, (size_t)H * DV, p.len, sV, tid);
   la_sums(a.geo, p, h, sG, tid);
   __syncthreads();
-  for (int j = 0; j <= i; ++j) {
+  if (const int j = m; j <= i) {
     const f4 x = la_dot_tile<DK>(sQ, sK, 16 * i, 16 * j, lane);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
@@ -244,7 +244,7 @@ __global__ __launch_bounds__(kThr) void la_fwd_kernel(LaFwdArgs<TIn> a) {
   for (int u = 0; u < 4; ++u) er[u] = la_exp(sG[16 * i + 4 * g + u + 1]);
   const float* S = a.N + p.ch * (size_t)(DK * DV);
   TIn* o = a.o + (p.row0 * H + h) * DV;
-  for (int t = 0; t < DV / 16; ++t) {
+  for (int t = m; t < DV / 16; t += kThrRows / 256) {
     f4 acc = la_state_tile<DK, DV>(sQ, S, 16 * i, 16 * t, f4{0.f, 0.f, 0.f, 0.f}, lane);
 #pragma unroll
     for (int u = 0; u < 4; ++u) acc[u] *= er[u];
@@ -258,45 +258,44 @@ __global__ __launch_bounds__(kThr) void la_fwd_kernel(LaFwdArgs<TIn> a) {
 }
 
 // ---- gradients -------------------------------------------------------------
+// waves as above
 template <int DK, int DV, typename TIn>
-__global__ __launch_bounds__(kThr) void la_bwd_kernel(LaBwdArgs<TIn> a) {
+__global__ __launch_bounds__(kThrRows) void la_bwd_kernel(LaBwdArgs<TIn> a) {
   __shared__ double sG[CH + 1];
-  __shared__ float sA[CH], sB[CH], sRow[CH], sCol[4][CH], sE[kThr / 64];
+  constexpr int NM = kThrRows / 256;
+  __shared__ float sA[NM][CH], sB[NM][CH], sRow[NM][CH], sCol[4][CH], sE[kThrRows / 64];
   extern __shared__ __align__(16) float smem[];
   float *sQ = smem, *sK = sQ + CH * (DK + 4), *sV = sK + CH * (DK + 4), *sD = sV + CH * (DV + 4);
   float* sP = sD + CH * (DV + 4);
-  const int tid = threadIdx.x, lane = tid & 63, i = tid >> 6, g = lane >> 4, l = lane & 15;
+  const int tid = threadIdx.x, lane = tid & 63, i = (tid >> 6) & 3, m = tid >> 8, g = lane >> 4, l = lane & 15;
   int h;
   ChunkPos p;
   if (!la_chunk(a.geo, blockIdx.x, h, p)) return;
   const int H = a.geo.H, HK = H / a.geo.G, hk = h / a.geo.G;
   const float scale = a.geo.scale;
-  la_tile<DK>(a.q + (p.row0 * HK + hk) * DK, (size_t)HK * DK, p.len, sQ, tid);
-  la_tile<DK>(a.k + (p.row0 * HK + hk) * DK, (size_t)HK * DK, p.len, sK, tid);
-  la_tile<DV>(a.v + (p.row0 * H + h) * DV, (size_t)H * DV, p.len, sV, tid);
-  la_tile<DV>(a.dout + (p.row0 * H + h) * DV, (size_t)H * DV, p.len, sD, tid);
+  la_tile<DK, kThrRows>(a.q + (p.row0 * HK + hk) * DK, (size_t)HK * DK, p.len, sQ, tid);
+  la_tile<DK, kThrRows>(a.k + (p.row0 * HK + hk) * DK, (size_t)HK * DK, p.len, sK, tid);
+  la_tile<DV, kThrRows>(a.v + (p.row0 * H + h) * DV, (size_t)H * DV, p.len, sV, tid);
+  la_tile<DV, kThrRows>(a.dout + (p.row0 * H + h) * DV, (size_t)H * DV, p.len, sD, tid);
   la_sums(a.geo, p, h, sG, tid);
-  for (int e = tid; e < 4 * CH; e += kThr) sCol[e / CH][e % CH] = 0.f;
+  for (int e = tid; e < 4 * CH; e += kThrRows) sCol[e / CH][e % CH] = 0.f;
   const float* S = a.N + p.ch * (size_t)(DK * DV);
   const float* dS = a.M + p.ch * (size_t)(DK * DV);
   float e0 = 0.f;
-  for (int e = 4 * tid; e < DK * DV; e += 4 * kThr) {
+  for (int e = 4 * tid; e < DK * DV; e += 4 * kThrRows) {
     const float4 x = ld4(S + e), y = ld4(dS + e);
     e0 += x.x * y.x + x.y * y.y + x.z * y.z + x.w * y.w;
   }
   e0 = row_sum(e0);
   e0 += row_partner16(e0, (lane & 16) != 0);
   e0 += row_partner32(e0, lane >= 32);
-  if (lane == 0) sE[i] = e0;
+  if (lane == 0) sE[tid >> 6] = e0;
   __syncthreads();
 
-  // scores of the wave's 16 query rows against every key row up to them
-  f4 wd[4];
+  // scores of 16 query rows against 16 key rows up to them
+  f4 wd = {0.f, 0.f, 0.f, 0.f};
   float rows[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    wd[j] = f4{0.f, 0.f, 0.f, 0.f};
-    if (j > i) continue;
+  if (const int j = m; j <= i) {
     f4 x = la_dot_tile<DK>(sQ, sK, 16 * i, 16 * j, lane);
     const f4 y = la_dot_tile<DV>(sD, sV, 16 * i, 16 * j, lane);
     float col = 0.f;
@@ -307,7 +306,7 @@ __global__ __launch_bounds__(kThr) void la_bwd_kernel(LaBwdArgs<TIn> a) {
       const float w = s < r ? scale * d * x[u] * y[u] : 0.f;
       rows[u] += w;
       col += w;
-      wd[j][u] = s <= r ? d * y[u] : 0.f;
+      wd[u] = s <= r ? d * y[u] : 0.f;
       sP[r * LP + s] = s <= r ? d * x[u] : 0.f;
     }
     col += row_partner16(col, (lane & 16) != 0);
@@ -317,7 +316,7 @@ __global__ __launch_bounds__(kThr) void la_bwd_kernel(LaBwdArgs<TIn> a) {
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     const float x = row_sum(rows[u]);
-    if (l == 0) sRow[16 * i + 4 * g + u] = x;
+    if (l == 0) sRow[m][16 * i + 4 * g + u] = x;
   }
   __syncthreads();
 
@@ -329,7 +328,7 @@ __global__ __launch_bounds__(kThr) void la_bwd_kernel(LaBwdArgs<TIn> a) {
   }
   // dv, and b_s = v_s . (exp(G_C - G_s) dS^T k_s)
   float dot[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int t = 0; t < DV / 16; ++t) {
+  for (int t = m; t < DV / 16; t += NM) {
     f4 inter = la_state_tile<DK, DV>(sK, dS, 16 * i, 16 * t, f4{0.f, 0.f, 0.f, 0.f}, lane);
     const f4 intra = la_cols_tile<DV>(sP, sD, i, 16 * t, f4{0.f, 0.f, 0.f, 0.f}, lane);
 #pragma unroll
@@ -343,18 +342,16 @@ __global__ __launch_bounds__(kThr) void la_bwd_kernel(LaBwdArgs<TIn> a) {
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     const float x = row_sum(dot[u]);
-    if (l == 0) sB[16 * i + 4 * g + u] = x;
+    if (l == 0) sB[m][16 * i + 4 * g + u] = x;
     dot[u] = 0.f;
   }
   __syncthreads();
+  if (m <= i)
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (j <= i)
-#pragma unroll
-      for (int u = 0; u < 4; ++u) sP[(16 * i + 4 * g + u) * LP + 16 * j + l] = wd[j][u];
+    for (int u = 0; u < 4; ++u) sP[(16 * i + 4 * g + u) * LP + 16 * m + l] = wd[u];
   __syncthreads();
   // dq, and a_r = q_r . (scale exp(G_r) S0 do_r); dk
-  for (int t = 0; t < DK / 16; ++t) {
+  for (int t = m; t < DK / 16; t += NM) {
     f4 qi = la_state_t_tile<DV>(sD, S, 16 * i, 16 * t, f4{0.f, 0.f, 0.f, 0.f}, lane);
     const f4 qa = la_rows_tile<DK>(sP, sK, i, 16 * t, f4{0.f, 0.f, 0.f, 0.f}, lane);
     const f4 ki = la_state_t_tile<DV>(sV, dS, 16 * i, 16 * t, f4{0.f, 0.f, 0.f, 0.f}, lane);
@@ -381,13 +378,14 @@ __global__ __launch_bounds__(kThr) void la_bwd_kernel(LaBwdArgs<TIn> a) {
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     const float x = row_sum(dot[u]);
-    if (l == 0) sA[16 * i + 4 * g + u] = x;
+    if (l == 0) sA[m][16 * i + 4 * g + u] = x;
   }
   __syncthreads();
   if (tid < 64) {
     // E + sum_{r>=t} a_r + sum_{s<t} (b_s + col_s - row_s)
-    double x = (double)sB[tid] + (((double)sCol[0][tid] + sCol[1][tid]) + ((double)sCol[2][tid] + sCol[3][tid])) - sRow[tid];
-    double y = sA[tid];
+    const auto all = [&](const float (&x)[4][CH]) { return ((double)x[0][tid] + x[1][tid]) + ((double)x[2][tid] + x[3][tid]); };
+    double x = all(sB) + all(sCol) - all(sRow);
+    double y = all(sA);
     const double own_x = x;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -395,7 +393,9 @@ __global__ __launch_bounds__(kThr) void la_bwd_kernel(LaBwdArgs<TIn> a) {
       if (tid >= o) x += px;
       if (tid + o < 64) y += py;
     }
-    const double E = (double)la_exp(sG[CH]) * (((double)sE[0] + sE[1]) + ((double)sE[2] + sE[3]));
+    double E = 0.0;
+    for (int w = 0; w < kThrRows / 64; ++w) E += sE[w];
+    E *= (double)la_exp(sG[CH]);
     if (tid < p.len) a.dg[(p.row0 + tid) * H + h] = (float)(E + y + (x - own_x));
   }
 }
@@ -443,7 +443,7 @@ hipError_t launch_la_state(const LaStateArgs<TIn>& a, bool rev, hipStream_t st) 
   const auto kernel = rev ? la_state_kernel<DK, DV, TIn, true> : la_state_kernel<DK, DV, TIn, false>;
   hipError_t e = la_lds(kernel, lds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernel, dim3(la_units(a.geo)), dim3(kThr), lds, st, a);
+  hipLaunchKernelGGL(kernel, dim3(la_units(a.geo)), dim3(kThrState), lds, st, a);
   return hipGetLastError();
 }
 
@@ -457,7 +457,7 @@ hipError_t launch_la_fwd(const LaFwdArgs<TIn>& a, hipStream_t st) {
   constexpr size_t lds = 4 * CH * (2 * (DK + 4) + DV + 4 + LP);
   hipError_t e = la_lds(la_fwd_kernel<DK, DV, TIn>, lds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((la_fwd_kernel<DK, DV, TIn>), dim3(la_units(a.geo)), dim3(kThr), lds, st, a);
+  hipLaunchKernelGGL((la_fwd_kernel<DK, DV, TIn>), dim3(la_units(a.geo)), dim3(kThrRows), lds, st, a);
   return hipGetLastError();
 }
 
@@ -466,7 +466,7 @@ hipError_t launch_la_bwd(const LaBwdArgs<TIn>& a, hipStream_t st) {
   constexpr size_t lds = 4 * CH * (2 * (DK + 4) + 2 * (DV + 4) + LP);
   hipError_t e = la_lds(la_bwd_kernel<DK, DV, TIn>, lds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((la_bwd_kernel<DK, DV, TIn>), dim3(la_units(a.geo)), dim3(kThr), lds, st, a);
+  hipLaunchKernelGGL((la_bwd_kernel<DK, DV, TIn>), dim3(la_units(a.geo)), dim3(kThrRows), lds, st, a);
   return hipGetLastError();
 }
 
