@@ -129,8 +129,8 @@ struct LaStepArgs {
 };
 
 template <int DK, int DV, typename TIn>
-hipError_t launch_la_state(const LaStateArgs<TIn>& a, bool rev, hipStream_t st);
-hipError_t launch_la_combine(const LaCombineArgs& a, hipStream_t st);
+hipError_t launch_la_state(const LaStateArgs<TIn>& fwd, const LaStateArgs<TIn>& rev, hipStream_t st);  // of N null: none
+hipError_t launch_la_combine(const LaCombineArgs& fwd, const LaCombineArgs& rev, hipStream_t st);  // of N null: none
 template <int DK, int DV, typename TIn>
 hipError_t launch_la_fwd(const LaFwdArgs<TIn>& a, hipStream_t st);
 template <int DK, int DV, typename TIn>
@@ -139,7 +139,7 @@ template <int DK, int DV, typename TIn>
 hipError_t launch_la_step(const LaStepArgs<TIn>& a, hipStream_t st);
 // out[r][h][c] = sum over the group's value heads of P[r][h G + j][c]
 template <typename TOut>
-hipError_t launch_la_group(const float* P, TOut* out, size_t rows, int Hk, int G, int D, hipStream_t st);
+hipError_t launch_la_group(const float* Pq, const float* Pk, TOut* dq, TOut* dk, size_t rows, int Hk, int G, int D, hipStream_t st);
 // dg[h] = sum over the rows of P[r][h]
 hipError_t launch_la_headsum(const float* P, float* dg, size_t rows, int H, hipStream_t st);
 

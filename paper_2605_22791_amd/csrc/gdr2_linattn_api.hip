@@ -144,14 +144,13 @@ hipError_t la_table(const gdr2_problem* p, const LaLayout& L, const int32_t* cu,
                              at<int>(ws, L.sord), st);
 }
 
-// the states that enter the chunks, from k and v (rev: the gradients of the end states, from q and dout)
+// the states that enter the chunks, from k and v, and the gradients of their end states, from q and
+// dout: those of them whose N is given
 template <int DK, int DV, typename TIn>
-hipError_t la_states(const LaGeo& geo, int ns, const void* x, const void* z, float* N, float* eGC, const float* init,
-                     float* fin, bool rev, hipStream_t st) {
-  const LaStateArgs<TIn> sa{geo, static_cast<const TIn*>(x), static_cast<const TIn*>(z), N, eGC};
-  hipError_t e = launch_la_state<DK, DV, TIn>(sa, rev, st);
-  if (e != hipSuccess) return e;
-  return launch_la_combine({geo, N, eGC, init, fin, ns, DK * DV, rev ? 1 : 0}, st);
+hipError_t la_states(const LaStateArgs<TIn>& fwd, const LaStateArgs<TIn>& rev, const LaCombineArgs& cf,
+                     const LaCombineArgs& cr, hipStream_t st) {
+  const hipError_t e = launch_la_state<DK, DV, TIn>(fwd, rev, st);
+  return e != hipSuccess ? e : launch_la_combine(cf, cr, st);
 }
 
 LaScanArgs la_scan_args(const LaLayout& L, const LaGeo& geo, int nseq, const void* q, const void* k, const void* v,
@@ -194,7 +193,8 @@ hipError_t la_fwd(const gdr2_problem* p, const LaLayout& L, const LaGeo& geo, in
     return e != hipSuccess ? e : launch_la_scan_fwd<DK, DV>(a, st);
   } else {
     float *N = at<float>(ws, L.N), *eGC = at<float>(ws, L.eGC);
-    hipError_t e = la_states<DK, DV, TIn>(geo, nseq > 0 ? nseq : p->B, k, v, N, eGC, S0, ST, false, st);
+    hipError_t e = la_states<DK, DV, TIn>({geo, static_cast<const TIn*>(k), static_cast<const TIn*>(v), N, eGC}, {},
+                                          {geo, N, eGC, S0, ST, nseq > 0 ? nseq : p->B, DK * DV, 0}, {}, st);
     if (e != hipSuccess) return e;
     return launch_la_fwd<DK, DV, TIn>({geo, static_cast<const TIn*>(q), static_cast<const TIn*>(k),
                                        static_cast<const TIn*>(v), static_cast<TIn*>(o), S0, N, eGC}, st);
@@ -237,15 +237,21 @@ hipError_t la_bwd(const gdr2_problem* p, const LaLayout& L, const LaGeo& geo, in
   } else {
     const int ns = nseq > 0 ? nseq : p->B;
     float *N = at<float>(ws, L.N), *M = at<float>(ws, L.M), *eGC = at<float>(ws, L.eGC);
-    if (!saved) e = la_states<DK, DV, TIn>(geo, ns, k, v, N, eGC, S0, nullptr, false, st);
-    if (e == hipSuccess) e = la_states<DK, DV, TIn>(geo, ns, q, dout, M, eGC, dST, d.dS0, true, st);
+    LaStateArgs<TIn> fwd{};
+    LaCombineArgs cf{};
+    if (!saved) {
+      fwd = {geo, static_cast<const TIn*>(k), static_cast<const TIn*>(v), N, eGC};
+      cf = {geo, N, eGC, S0, nullptr, ns, DK * DV, 0};
+    }
+    e = la_states<DK, DV, TIn>(fwd, {geo, static_cast<const TIn*>(q), static_cast<const TIn*>(dout), M, eGC}, cf,
+                               {geo, M, eGC, dST, d.dS0, ns, DK * DV, 1}, st);
     if (e != hipSuccess) return e;
     e = launch_la_bwd<DK, DV, TIn>({geo, static_cast<const TIn*>(q), static_cast<const TIn*>(k),
                                     static_cast<const TIn*>(v), static_cast<const TIn*>(dout), static_cast<TIn*>(d.dq),
                                     static_cast<TIn*>(d.dk), static_cast<TIn*>(d.dv), Pq, Pk, dg, N, M, eGC}, st);
   }
-  if (e == hipSuccess && geo.G > 1) e = launch_la_group<TIn>(Pq, static_cast<TIn*>(d.dq), rows, geo.H / geo.G, geo.G, DK, st);
-  if (e == hipSuccess && geo.G > 1) e = launch_la_group<TIn>(Pk, static_cast<TIn*>(d.dk), rows, geo.H / geo.G, geo.G, DK, st);
+  if (e == hipSuccess && geo.G > 1)
+    e = launch_la_group<TIn>(Pq, Pk, static_cast<TIn*>(d.dq), static_cast<TIn*>(d.dk), rows, geo.H / geo.G, geo.G, DK, st);
   if (e == hipSuccess && geo.per_head) e = launch_la_headsum(dg, d.dg, rows, geo.H, st);
   return e;
 }

@@ -142,10 +142,9 @@ __device__ __forceinline__ f4 la_cols_tile(const float* P, const float* Z, int j
 
 // ---- every chunk's contribution to the state -------------------------------
 template <int DK, int DV, typename TIn, bool REV>
-__global__ __launch_bounds__(kThrState) void la_state_kernel(LaStateArgs<TIn> a) {
+__device__ __forceinline__ void la_state(const LaStateArgs<TIn>& a, float* smem) {
   __shared__ double sG[CH + 1];
   __shared__ float sW[CH];
-  extern __shared__ __align__(16) float smem[];
   float *sX = smem, *sZ = sX + CH * (DK + 4);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int h;
@@ -178,10 +177,21 @@ __global__ __launch_bounds__(kThrState) void la_state_kernel(LaStateArgs<TIn> a)
   }
 }
 
+// Of the states, their gradients, or (grid y) the two side by side.
+template <int DK, int DV, typename TIn>
+__global__ __launch_bounds__(kThrState) void la_state_kernel(LaStateArgs<TIn> fwd, LaStateArgs<TIn> rev) {
+  extern __shared__ __align__(16) float smem[];
+  if (blockIdx.y == 0 && fwd.N)
+    la_state<DK, DV, TIn, false>(fwd, smem);
+  else
+    la_state<DK, DV, TIn, true>(rev, smem);
+}
+
 // ---- the states that enter the chunks --------------------------------------
 // A thread takes four elements through its sequence; eight chunks' loads are in
 // flight at a time.
-__global__ __launch_bounds__(kThr) void la_combine_kernel(LaCombineArgs a) {
+__global__ __launch_bounds__(kThr) void la_combine_kernel(LaCombineArgs fwd, LaCombineArgs rev) {
+  const LaCombineArgs a = blockIdx.y == 0 && fwd.N ? fwd : rev;
   constexpr int AHEAD = 8;
   const int per = a.size / (4 * kThr);
   const int q = blockIdx.x / per, e = ((blockIdx.x % per) * kThr + threadIdx.x) * 4;
@@ -402,7 +412,10 @@ __global__ __launch_bounds__(kThrRows) void la_bwd_kernel(LaBwdArgs<TIn> a) {
 
 // ---- sums over a group's value heads, and over the tokens ------------------
 template <typename TOut>
-__global__ __launch_bounds__(256) void la_group_kernel(const float* P, TOut* out, size_t n4, int G, int D) {
+__global__ __launch_bounds__(256) void la_group_kernel(const float* Pq, const float* Pk, TOut* dq, TOut* dk, size_t n4, int G,
+                                                       int D) {
+  const float* P = blockIdx.y ? Pk : Pq;
+  TOut* out = blockIdx.y ? dk : dq;
   const size_t stride = (size_t)gridDim.x * blockDim.x;
   for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < n4; i += stride) {
     const size_t c = 4 * i % D, rh = 4 * i / D;
@@ -438,17 +451,19 @@ hipError_t la_lds(K kernel, size_t bytes) {
 }  // namespace
 
 template <int DK, int DV, typename TIn>
-hipError_t launch_la_state(const LaStateArgs<TIn>& a, bool rev, hipStream_t st) {
+hipError_t launch_la_state(const LaStateArgs<TIn>& fwd, const LaStateArgs<TIn>& rev, hipStream_t st) {
   constexpr size_t lds = 4 * CH * (DK + DV + 8);
-  const auto kernel = rev ? la_state_kernel<DK, DV, TIn, true> : la_state_kernel<DK, DV, TIn, false>;
-  hipError_t e = la_lds(kernel, lds);
+  hipError_t e = la_lds(la_state_kernel<DK, DV, TIn>, lds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernel, dim3(la_units(a.geo)), dim3(kThrState), lds, st, a);
+  hipLaunchKernelGGL((la_state_kernel<DK, DV, TIn>), dim3(la_units((fwd.N ? fwd : rev).geo), fwd.N && rev.N ? 2 : 1),
+                     dim3(kThrState), lds, st, fwd, rev);
   return hipGetLastError();
 }
 
-hipError_t launch_la_combine(const LaCombineArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL(la_combine_kernel, dim3((unsigned)(a.nseq * a.geo.H * (a.size / (4 * kThr)))), dim3(kThr), 0, st, a);
+hipError_t launch_la_combine(const LaCombineArgs& fwd, const LaCombineArgs& rev, hipStream_t st) {
+  const LaCombineArgs& a = fwd.N ? fwd : rev;
+  hipLaunchKernelGGL(la_combine_kernel, dim3((unsigned)(a.nseq * a.geo.H * (a.size / (4 * kThr))), fwd.N && rev.N ? 2 : 1),
+                     dim3(kThr), 0, st, fwd, rev);
   return hipGetLastError();
 }
 
@@ -471,14 +486,14 @@ hipError_t launch_la_bwd(const LaBwdArgs<TIn>& a, hipStream_t st) {
 }
 
 template <typename TOut>
-hipError_t launch_la_group(const float* P, TOut* out, size_t rows, int Hk, int G, int D, hipStream_t st) {
+hipError_t launch_la_group(const float* Pq, const float* Pk, TOut* dq, TOut* dk, size_t rows, int Hk, int G, int D, hipStream_t st) {
   const size_t n4 = rows * Hk * (size_t)D / 4, blocks = (n4 + 255) / 256;
-  hipLaunchKernelGGL(la_group_kernel<TOut>, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), 0, st, P, out,
-                     n4, G, D);
+  hipLaunchKernelGGL(la_group_kernel<TOut>, dim3((unsigned)(blocks < 16384 ? blocks : 16384), 2), dim3(256), 0, st, Pq, Pk,
+                     dq, dk, n4, G, D);
   return hipGetLastError();
 }
-template hipError_t launch_la_group<float>(const float*, float*, size_t, int, int, int, hipStream_t);
-template hipError_t launch_la_group<bf16_t>(const float*, bf16_t*, size_t, int, int, int, hipStream_t);
+template hipError_t launch_la_group<float>(const float*, const float*, float*, float*, size_t, int, int, int, hipStream_t);
+template hipError_t launch_la_group<bf16_t>(const float*, const float*, bf16_t*, bf16_t*, size_t, int, int, int, hipStream_t);
 
 hipError_t launch_la_headsum(const float* P, float* dg, size_t rows, int H, hipStream_t st) {
   hipLaunchKernelGGL(la_headsum_kernel, dim3((unsigned)H), dim3(1024), 0, st, P, dg, rows, H);
@@ -486,7 +501,7 @@ hipError_t launch_la_headsum(const float* P, float* dg, size_t rows, int H, hipS
 }
 
 #define GDR2_LA_INST(DK, DV, T)                                                                   \
-  template hipError_t launch_la_state<DK, DV, T>(const LaStateArgs<T>&, bool, hipStream_t);       \
+  template hipError_t launch_la_state<DK, DV, T>(const LaStateArgs<T>&, const LaStateArgs<T>&, hipStream_t); \
   template hipError_t launch_la_fwd<DK, DV, T>(const LaFwdArgs<T>&, hipStream_t);                 \
   template hipError_t launch_la_bwd<DK, DV, T>(const LaBwdArgs<T>&, hipStream_t);
 #define GDR2_LA_INST4(T) \
