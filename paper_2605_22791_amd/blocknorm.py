@@ -39,14 +39,16 @@ def _inputs(y, w_post, gate, x, res_scale, w_pre, eps):
         raise ValueError("y: expected rows along the last axis")
     D, dev = y.shape[-1], y.device
     code = _dtype_code(y)
-    _require("y", y, y.shape, y.dtype, dev)
-    _require("gate", gate, y.shape, y.dtype, dev)
-    if x is not None and x.dtype != y.dtype and x.dtype != torch.float32:
-        raise TypeError(f"x: {x.dtype}, expected {y.dtype} or torch.float32")
-    stream = y.dtype if x is None else x.dtype
-    _require("x", x, y.shape, stream, dev)
-    for name, w in (("w_post", w_post), ("res_scale", res_scale), ("w_pre", w_pre)):
-        _require(name, w, (D,), torch.float32, dev)
+    shape, dt = y.shape, y.dtype
+    _require("y", y, shape, dt)
+    _require("gate", gate, shape, dt, dev)
+    if x is not None and x.dtype != dt and x.dtype != torch.float32:
+        raise TypeError(f"x: {x.dtype}, expected {dt} or torch.float32")
+    stream = dt if x is None else x.dtype
+    _require("x", x, shape, stream, dev)
+    _require("w_post", w_post, (D,), torch.float32, dev)
+    _require("res_scale", res_scale, (D,), torch.float32, dev)
+    _require("w_pre", w_pre, (D,), torch.float32, dev)
     rows = y.numel() // D if D else 0
     return Gdr2Blocknorm(rows, D, code, 1 if stream is torch.float32 else 0, float(eps)), stream
 
@@ -64,11 +66,11 @@ def gdr2_blocknorm_fwd(y, *, w_post=None, gate=None, x=None, res_scale=None, w_p
     torch = _torch()
     p, stream = _inputs(y, w_post, gate, x, res_scale, w_pre, eps)
     if h is None and want_h:
-        h = torch.empty(y.shape, dtype=stream, device=y.device)
+        h = torch.empty_like(y, dtype=stream)
     else:
         _require("h", h, y.shape, stream, y.device)
     if n is None and w_pre is not None:
-        n = torch.empty(y.shape, dtype=y.dtype, device=y.device)
+        n = torch.empty_like(y)
     elif n is not None and w_pre is None:
         raise ValueError("n: given, but the call has no w_pre")
     else:
