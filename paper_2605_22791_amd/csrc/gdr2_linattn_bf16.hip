@@ -20,8 +20,9 @@
 //     X, Z there, Y's place free:  load Y;  X St, Z fragments
 //     Y there:                     scores, the decays of the next chunk
 //     P there, X, Z done with:     load the next X, Z;  P Z, output, update
-// Vector instructions bound the scans: one takes 4 cycles of a SIMD's issue and an MFMA 8 (of 16
-// that it is busy for) when several waves share it, so what counts is how many there are.
+// What counts is how many instructions there are: a vector one takes 4 cycles of a SIMD's issue
+// and an MFMA 8 (of 16 that it is busy for) when waves share it, and at these rates the chip
+// draws its power: its clock falls to 1.6 GHz in the long scans, from 2.2 in short ones.
 // Two workgroups a CU (80 KB of LDS each) fill each other's gaps.
 //
 // Precision: inputs are exact bf16 operands.  fp32 operands are split: what only feeds bf16
@@ -29,9 +30,10 @@
 // (S_T, dS0 are fp32), and the state and scores where the decays' gradient reads the
 // product, into three (24 bits).
 //
-// Measured, 8 x 4096 tokens, 16 heads of 128 x 128, four segments a sequence: forward scan 151 us
-// (537 MB, 3.6 TB/s), segment states 68 and 64 us, the three gradients 574 us, decays' gradient
-// 23 us.
+// Measured, 8 x 4096 tokens, 16 heads of 128 x 128, four segments a sequence: forward scan 147 us
+// (537 MB, 3.7 TB/s; 129 with every load from the same place), segment states 70 and 67 us, the
+// three gradients 527 us (458; 454 with two parts for three throughout, which costs the decays'
+// gradient its 1e-6), the decays' gradient 24 us.
 
 #include "gdr2_linattn.hpp"
 #include "gdr2_bf16.hpp"
@@ -493,13 +495,13 @@ __device__ __forceinline__ f4 la_score(const unsigned char* Am, const unsigned c
 }
 
 // Factors scale D_rs of a tile: ROWS_S, the lane's four values are s (r = r0 + c, one a lane), else
-// r (s = s0 + c).  i, j: the blocks of r and s; on the diagonal itself D is 1.
-template <bool ROWS_S>
+// r (s = s0 + c).  i, j: the blocks of r and s, DIAG: the same one; on the diagonal itself D is 1.
+template <bool ROWS_S, bool DIAG>
 __device__ __forceinline__ f4 la_decay_tile(const LaTab& t, int i, int j, int lane, float scale) {
   lane = la_new(lane);
   const int g = lane >> 4, c = lane & 15;
   f4 d;
-  if (i != j) {
+  if constexpr (!DIAG) {
     if constexpr (ROWS_S) {
       const float l = t.L[16 * i + c];
       d = *reinterpret_cast<const f4*>(&t.R[i - 1][16 * j + 4 * g]) * l;
@@ -519,15 +521,11 @@ __device__ __forceinline__ f4 la_decay_tile(const LaTab& t, int i, int j, int la
   return d;
 }
 
-// The lower tiles (i, j <= i) of a chunk's scores over the waves, fewer for the last, which forms
-// the decays of the next chunk.
-template <int NW>
-__device__ __forceinline__ int la_tiles(int wave) { return NW == 4 ? (wave < 3 ? 3 : 1) : (wave < 1 ? 6 : 4); }
-template <int NW>
-__device__ __forceinline__ void la_tile_of(int wave, int m, int& i, int& j) {
-  const int n = (NW == 4 ? 3 : 6) * wave + m;  // (3,0) (3,1) (3,2) (2,0) (2,1) (1,0) (0,0) (1,1) (2,2) (3,3)
-  i = n < 3 ? 3 : n < 5 ? 2 : n < 6 ? 1 : n - 6;
-  j = n < 3 ? n : n < 5 ? n - 3 : n < 6 ? 0 : n - 6;
+// The lower tiles (i, j <= i) of a chunk's scores, the six off the diagonal first: blocks of tile n
+__device__ __forceinline__ void la_tile_of(int n, int& i, int& j) {
+  // (3,0) (3,1) (3,2) (2,0) (2,1) (1,0)
+  i = n < 3 ? 3 : n < 5 ? 2 : 1;
+  j = n < 3 ? n : n < 5 ? n - 3 : 0;
 }
 
 // Score tiles in LDS, 512 bytes each (16 rows of the output, 16 columns that the product with Z
@@ -758,6 +756,31 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
       (ROLE == kLaDq ? a.ca : a.cb)[((size_t)unit * (a.segs.seg_tokens / CH) + at(n)) * 16 + lane] = y;
     }
   };
+  const auto scores = [&](auto count, auto diag, int n0, const LaTab& t) {
+    constexpr int N = decltype(count)::value;
+    constexpr bool DIAG = decltype(diag)::value;
+    f4 x[N];
+    int io[N], jz[N];  // output's and Z's block
+#pragma unroll
+    for (int m = 0; m < N; ++m) {
+      int i = n0 + m, j = i;
+      if (!DIAG) la_tile_of(n0 + m, i, j);
+      io[m] = REV ? j : i, jz[m] = REV ? i : j;
+      x[m] = la_score<A>(sY, sX, ax, jz[m], io[m]) * la_decay_tile<!REV, DIAG>(t, i, j, lane, scale);
+    }
+#pragma unroll
+    for (int m = 0; m < N; ++m) {
+      if constexpr (SUMS && DIAG) {
+        // the diagonal cancels between a and b: it is kept out of both and added to the output by itself
+        const int u0 = la_new(c - 4 * g);
+        if ((unsigned)u0 < 4u)
+          sDiag[16 * io[m] + c] = u0 < 2 ? (u0 == 0 ? x[m][0] : x[m][1]) : (u0 == 2 ? x[m][2] : x[m][3]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[m][u] = u == u0 ? 0.f : x[m][u];
+      }
+      la_split4<PARTS>(sP + la_ptile<REV>(io[m], jz[m]) * 256 + 16 * c + 4 * g, kLaScores, x[m]);
+    }
+  };
   for (int n = 0; n < nc; ++n) {
     __syncthreads();  // X and Z are there; Y, P and the terms of the chunk before are done with
     lx.load(Y, sx, lds + C::OFF_Y, wave);
@@ -793,26 +816,18 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
         zr[i] = la_ld16(sZ + ax.out + 16 * i * kLaRow);
       }
     }
-    // scores: rows of the output by rows of Z, four of the latter a lane
-#pragma unroll
-    for (int m = 0; m < la_tiles<NW>(0); ++m) {
-      if (m < la_tiles<NW>(wave)) {
-        int i, j;
-        la_tile_of<NW>(wave, m, i, j);
-        const int io = REV ? j : i, jz = REV ? i : j;  // output's and Z's block
-        f4 x = la_score<A>(sY, sX, ax, jz, io);
-        x *= la_decay_tile<!REV>(t, i, j, lane, scale);
-        if constexpr (SUMS) {
-          // the diagonal cancels between a and b: it is kept out of both and added to the output by itself
-          if (i == j) {
-            const int u0 = la_new(c - 4 * g);
-            if ((unsigned)u0 < 4u) sDiag[16 * i + c] = u0 < 2 ? (u0 == 0 ? x[0] : x[1]) : (u0 == 2 ? x[2] : x[3]);
-#pragma unroll
-            for (int u = 0; u < 4; ++u) x[u] = u == u0 ? 0.f : x[u];
-          }
-        }
-        la_split4<PARTS>(sP + la_ptile<REV>(io, jz) * 256 + 16 * c + 4 * g, kLaScores, x);
-      }
+    // scores: rows of the output by rows of Z, four of the latter a lane.  The first half of the waves
+    // shares the tiles off the diagonal, the others have those on it, the last but one (and the
+    // decays of the next chunk).  A wave's tiles run side by side.
+    if (wave < NW / 2) {
+      scores(std::integral_constant<int, 12 / NW>{}, std::false_type{}, 12 / NW * wave, t);
+    } else if constexpr (NW == 4) {
+      if (wave == 2)
+        scores(std::integral_constant<int, 3>{}, std::true_type{}, 0, t);
+      else
+        scores(std::integral_constant<int, 1>{}, std::true_type{}, 3, t);
+    } else {
+      scores(std::integral_constant<int, 4>{}, std::true_type{}, 0, t);
     }
     if (more && wave == TW) {
       la_tables(graw, rows(n + 1), tab[(n + 1) & 1], lane, scale);
@@ -904,7 +919,6 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
       }
     }
     if constexpr (SUMS) sA[wave * CH + lane] = la_sum4(sum);
-    __builtin_amdgcn_sched_barrier(0);
     st.template update<C::UPARTS>(sY, ax, z, REV ? t.E : t.T, lane);
     if constexpr (ROLE == kLaDq) {
       if ((n + 1) % kLaAnchor == 0 || !more)
