@@ -10,7 +10,12 @@
 // A row belongs to LPR lanes of eight elements each; the weights stay in the
 // lanes' registers over the rows that a workgroup takes in turn, and so do the
 // sums of the weights' gradients, which leave once per workgroup and are added
-// by a second launch in a fixed order.
+// by a second launch in a fixed order.  The backward loads a row ahead.
+//
+// Measured: 524288 bf16 rows of 128 with norm and gate, forward 86 us (403 MB, 4.7
+// TB/s), backward 134 us (671 MB, 5.0 TB/s; 212 without the row ahead and in the
+// registers of the full form); 32768 rows of 2048, everything, fp32 stream: 166 us
+// (0.94 GB) and 336 us (1.47 GB, 4.4 TB/s); 1999 fp32 rows of 1155: 11 and 19 us.
 
 #include "gdr2_blocknorm.hpp"
 #include "gdr2_bf16.hpp"
@@ -396,7 +401,7 @@ hipError_t norm_dispatch(int D, F&& f) {
 }  // namespace
 
 // Workgroups of a backward call, as many as are resident together: four waves a SIMD of the form
-// without x, c and w_pre, two of the other (at 1024 for both, rows of 2048 took 382 us for 340)
+// without x, c and w_pre, two of the other (1024 of the latter, rows of 2048, took 382 us for 336)
 int norm_bwd_blocks(int64_t rows, int D, bool rest) {
   const int rpb = norm_rows_per_block(D);
   const int64_t n = (rows + rpb - 1) / rpb, most = rest ? 512 : 1024;
