@@ -658,8 +658,7 @@ struct LaCfg {
   static constexpr bool REV = ROLE == kLaDv || ROLE == kLaDk, TR = ROLE == kLaDq || ROLE == kLaDk;  // state transposed
   static constexpr bool SUMS = ROLE == kLaDq || ROLE == kLaDv;  // gives a term of the decays' gradient
   static constexpr int A = TR ? DV : DK, B = TR ? DK : DV, NW = B / 32;
-  // parts of the state and the scores in products, and of the decayed Z
-  static constexpr int PARTS = SUMS ? 3 : 2, UPARTS = ROLE == kLaDk ? 2 : 3;
+  static constexpr int PARTS = SUMS ? 3 : 2;  // of the state and the scores in products
   static constexpr int OFF_Y = la_bytes(A), OFF_Z = 2 * OFF_Y, OFF_P = OFF_Z + la_bytes(B);
   static constexpr int OFF_S = OFF_P + PARTS * kLaScores * 2, OFF_T = OFF_S + NW * 2048;
   static constexpr int OFF_A = OFF_T + 2 * (int)sizeof(LaTab);
@@ -756,6 +755,9 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
       (ROLE == kLaDq ? a.ca : a.cb)[((size_t)unit * (a.segs.seg_tokens / CH) + at(n)) * 16 + lane] = y;
     }
   };
+  // Parts of the decayed Z: two where the state feeds nothing but bf16 outputs (dk; o, but for
+  // the segment that leaves S_T: the states between segments come of their own pass)
+  const bool exact = SUMS || (ROLE == kLaO && un.last && a.ST != nullptr);
   const auto scores = [&](auto count, auto diag, int n0, const LaTab& t) {
     constexpr int N = decltype(count)::value;
     constexpr bool DIAG = decltype(diag)::value;
@@ -818,16 +820,27 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
     }
     // scores: rows of the output by rows of Z, four of the latter a lane.  The first half of the waves
     // shares the tiles off the diagonal, the others have those on it, the last but one (and the
-    // decays of the next chunk).  A wave's tiles run side by side.
-    if (wave < NW / 2) {
-      scores(std::integral_constant<int, 12 / NW>{}, std::false_type{}, 12 / NW * wave, t);
-    } else if constexpr (NW == 4) {
-      if (wave == 2)
-        scores(std::integral_constant<int, 3>{}, std::true_type{}, 0, t);
+    // decays of the next chunk).  Up to three of a wave's tiles run side by side.
+    const auto off = std::false_type{};
+    const auto diagonal = std::true_type{};
+    const auto one = std::integral_constant<int, 1>{};
+    const auto two = std::integral_constant<int, 2>{};
+    const auto three = std::integral_constant<int, 3>{};
+    if constexpr (NW == 4) {
+      if (wave < 2)
+        scores(three, off, 3 * wave, t);
+      else if (wave == 2)
+        scores(three, diagonal, 0, t);
       else
-        scores(std::integral_constant<int, 1>{}, std::true_type{}, 3, t);
+        scores(one, diagonal, 3, t);
     } else {
-      scores(std::integral_constant<int, 4>{}, std::true_type{}, 0, t);
+      if (wave == 0) {
+        scores(three, off, 0, t);
+        scores(three, off, 3, t);
+      } else {
+        scores(two, diagonal, 0, t);
+        scores(two, diagonal, 2, t);
+      }
     }
     if (more && wave == TW) {
       la_tables(graw, rows(n + 1), tab[(n + 1) & 1], lane, scale);
@@ -919,7 +932,10 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
       }
     }
     if constexpr (SUMS) sA[wave * CH + lane] = la_sum4(sum);
-    st.template update<C::UPARTS>(sY, ax, z, REV ? t.E : t.T, lane);
+    if (exact)
+      st.template update<3>(sY, ax, z, REV ? t.E : t.T, lane);
+    else
+      st.template update<2>(sY, ax, z, REV ? t.E : t.T, lane);
     if constexpr (ROLE == kLaDq) {
       if ((n + 1) % kLaAnchor == 0 || !more)
         st.template store<B, TR>(a.aS + ((size_t)unit * a.anchors + n / kLaAnchor) * (DK * DV), lane, wave);
