@@ -27,12 +27,12 @@
 //
 // Precision: inputs are exact bf16 operands.  fp32 operands are split: what only feeds bf16
 // outputs into two parts (16 bits, against the outputs' 8); the decayed Z of the update
-// (S_T, dS0 are fp32), and the state and scores where the decays' gradient reads the
-// product, into three (24 bits).
+// (S_T, dS0 are fp32; of the forward's segments, in those that leave S_T), and the state and
+// scores where the decays' gradient reads the product, into three (24 bits).
 //
-// Measured, 8 x 4096 tokens, 16 heads of 128 x 128, four segments a sequence: forward scan 147 us
-// (537 MB, 3.7 TB/s; 129 with every load from the same place), segment states 70 and 67 us, the
-// three gradients 527 us (458; 454 with two parts for three throughout, which costs the decays'
+// Measured, 8 x 4096 tokens, 16 heads of 128 x 128, four segments a sequence: forward scan 138 us
+// (537 MB, 3.9 TB/s), segment states 68 and 65 us, the three gradients 511 to 527 us (458 with
+// every load from the same place; 454 with two parts for three throughout, which costs the decays'
 // gradient its 1e-6), the decays' gradient 24 us.
 
 #include "gdr2_linattn.hpp"
