@@ -81,9 +81,12 @@ struct LaCombineArgs {
 // A sequence is cut into segments of seg_tokens tokens (a multiple of 64; an empty
 // sequence has one without tokens); slot = sequence * nseg + segment, or, packed, an
 // entry of a table: first token, tokens and sequence of every slot, and the first
-// slot of every sequence.
+// slot of every sequence.  Up to 64 sequences need no table: a wave looks a slot up in
+// the offsets, a sequence a lane (nine prompts of 8192 tokens in all: 75 us a
+// forward call, 77 with the launch that writes the table and the reads of it).
 struct LaSegs {
   const int *t0 = nullptr, *len = nullptr, *seq = nullptr, *off = nullptr;  // packed only
+  const int* cu = nullptr;  // packed, up to 64 sequences: in place of the table
   int nseq, nseg, nslot, seg_tokens;
 };
 

@@ -137,6 +137,7 @@ LaGeo la_geo(const gdr2_problem* p, const LaLayout& L, int decay, const int32_t*
 
 hipError_t la_table(const gdr2_problem* p, const LaLayout& L, const int32_t* cu, int nseq, void* ws, hipStream_t st) {
   if (nseq == 0) return hipSuccess;
+  if (p->dtype == GDR2_BF16 && nseq <= 64) return hipSuccess;
   if (p->dtype == GDR2_BF16)
     return launch_la_segtable(cu, L.segs, p->T, at<int>(ws, L.st0), at<int>(ws, L.slen), at<int>(ws, L.sseq),
                               at<int>(ws, L.soff), st);
@@ -153,12 +154,14 @@ hipError_t la_states(const LaStateArgs<TIn>& fwd, const LaStateArgs<TIn>& rev, c
   return e != hipSuccess ? e : launch_la_combine(cf, cr, st);
 }
 
-LaScanArgs la_scan_args(const LaLayout& L, const LaGeo& geo, int nseq, const void* q, const void* k, const void* v,
+LaScanArgs la_scan_args(const LaLayout& L, const LaGeo& geo, const int32_t* cu, int nseq, const void* q, const void* k, const void* v,
                         const float* S0, void* ws) {
   LaScanArgs a{};
   a.geo = geo;
   a.segs = L.segs;
-  if (nseq > 0) {
+  if (nseq > 0 && nseq <= 64) {
+    a.segs.cu = cu;
+  } else if (nseq > 0) {
     a.segs.t0 = at<int>(ws, L.st0);
     a.segs.len = at<int>(ws, L.slen);
     a.segs.seq = at<int>(ws, L.sseq);
@@ -183,10 +186,10 @@ hipError_t la_seg_states(const LaScanArgs& a, bool rev, hipStream_t st) {
 }
 
 template <int DK, int DV, typename TIn>
-hipError_t la_fwd(const gdr2_problem* p, const LaLayout& L, const LaGeo& geo, int nseq, const void* q, const void* k,
+hipError_t la_fwd(const gdr2_problem* p, const LaLayout& L, const LaGeo& geo, const int32_t* cu, int nseq, const void* q, const void* k,
                   const void* v, const float* S0, void* o, float* ST, void* ws, hipStream_t st) {
   if constexpr (std::is_same<TIn, bf16_t>::value) {
-    LaScanArgs a = la_scan_args(L, geo, nseq, q, k, v, S0, ws);
+    LaScanArgs a = la_scan_args(L, geo, cu, nseq, q, k, v, S0, ws);
     a.o = static_cast<bf16_t*>(o);
     a.ST = ST;
     hipError_t e = L.multi ? la_seg_states<DK, DV>(a, false, st) : hipSuccess;
@@ -207,7 +210,7 @@ struct LaGrads {
 };
 
 template <int DK, int DV, typename TIn>
-hipError_t la_bwd(const gdr2_problem* p, const LaLayout& L, const LaGeo& geo, int nseq, const void* q, const void* k,
+hipError_t la_bwd(const gdr2_problem* p, const LaLayout& L, const LaGeo& geo, const int32_t* cu, int nseq, const void* q, const void* k,
                   const void* v, const float* S0, const void* dout, const float* dST, const LaGrads& d, void* ws,
                   bool saved, hipStream_t st) {
   const size_t rows = (size_t)p->B * p->T;
@@ -215,7 +218,7 @@ hipError_t la_bwd(const gdr2_problem* p, const LaLayout& L, const LaGeo& geo, in
   float* dg = geo.per_head ? at<float>(ws, L.dg) : d.dg;
   hipError_t e = hipSuccess;
   if constexpr (std::is_same<TIn, bf16_t>::value) {
-    LaScanArgs a = la_scan_args(L, geo, nseq, q, k, v, S0, ws);
+    LaScanArgs a = la_scan_args(L, geo, cu, nseq, q, k, v, S0, ws);
     a.dout = static_cast<const bf16_t*>(dout);
     a.dST = dST;
     a.dS0 = d.dS0;
@@ -311,7 +314,8 @@ gdr2_status gdr2_linattn_fwd(const gdr2_problem* p, int32_t decay, const int32_t
   hipError_t e = la_table(p, L, cu, n_seqs, ws, stream);
   if (e == hipSuccess)
     e = la_dispatch(p, [&](auto dk, auto dv, auto t) {
-      return la_fwd<decltype(dk)::value, decltype(dv)::value, decltype(t)>(p, L, geo, n_seqs, q, k, v, S0, o, S_T, ws, stream);
+      return la_fwd<decltype(dk)::value, decltype(dv)::value, decltype(t)>(p, L, geo, cu, n_seqs, q, k, v, S0, o, S_T, ws,
+                                                                           stream);
     });
   return hip_status(e, stream);
 }
@@ -332,8 +336,8 @@ gdr2_status gdr2_linattn_bwd(const gdr2_problem* p, int32_t decay, const int32_t
   hipError_t e = saved ? hipSuccess : la_table(p, L, cu, n_seqs, ws, stream);
   if (e == hipSuccess)
     e = la_dispatch(p, [&](auto ck, auto cv, auto t) {
-      return la_bwd<decltype(ck)::value, decltype(cv)::value, decltype(t)>(p, L, geo, n_seqs, q, k, v, S0, dout, dS_T, d, ws,
-                                                                           saved != 0, stream);
+      return la_bwd<decltype(ck)::value, decltype(cv)::value, decltype(t)>(p, L, geo, cu, n_seqs, q, k, v, S0, dout, dS_T, d,
+                                                                           ws, saved != 0, stream);
     });
   return hip_status(e, stream);
 }

@@ -50,10 +50,46 @@ struct LaUnit {
   bool first, last;
 };
 
+// Sequence `lane` of up to 64: its tokens a to b, its slots first to behind (a whole wave calls).
+struct LaSpan {
+  int a, b, first, behind;
+  __device__ __forceinline__ LaSpan(const LaSegs& s, int T) {
+    const int lane = threadIdx.x & 63;
+    a = b = 0;
+    int n = 0;
+    if (lane < s.nseq) {
+      a = min(max(s.cu[lane], 0), T);
+      b = min(max(s.cu[lane + 1], a), T);
+      n = max(1, (b - a + s.seg_tokens - 1) / s.seg_tokens);
+    }
+    behind = n;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(behind, o);
+      if (lane >= o) behind += y;
+    }
+    first = behind - n;
+  }
+};
+
 // Segment `slot`; false past the last one in use (uniform).  Table entries are kept in range
 // whatever a workspace holds.
 __device__ __forceinline__ bool la_unit(const LaSegs& s, int T, int slot, LaUnit& u) {
   u.slot = slot;
+  if (s.cu) {
+    const LaSpan x(s, T);
+    const int lane = threadIdx.x & 63;
+    u.seq = __popcll(__ballot(lane < s.nseq && x.behind <= slot));
+    if (slot >= s.nslot || u.seq >= s.nseq) return false;
+    const int a = __builtin_amdgcn_readlane(x.a, u.seq), b = __builtin_amdgcn_readlane(x.b, u.seq);
+    const int first = __builtin_amdgcn_readlane(x.first, u.seq), behind = __builtin_amdgcn_readlane(x.behind, u.seq);
+    const int t0 = a + (slot - first) * s.seg_tokens;
+    u.row0 = (size_t)t0;
+    u.len = max(0, min(s.seg_tokens, b - t0));
+    u.first = slot == first;
+    u.last = slot + 1 == behind;
+    return true;
+  }
   if (s.off == nullptr) {
     if (slot >= s.nslot) return false;
     const int i = slot % s.nseg;
@@ -617,11 +653,15 @@ __global__ __launch_bounds__(2 * DV, 2) void la_segstate_kernel(LaScanArgs a) {
 // The states behind the segments (rev: the gradients before them), in the place of their
 // contributions: what the chain's next segment starts from.
 __global__ __launch_bounds__(256) void la_segcombine_kernel(LaScanArgs a, int size, int rev) {
-  constexpr int AHEAD = 8;
+  constexpr int AHEAD = 16;
   const int H = a.geo.H, per = size / 1024;
   const int q = blockIdx.x / per, e = ((blockIdx.x % per) * 256 + threadIdx.x) * 4, s = q / H, h = q % H;
   int c0 = s * a.segs.nseg, c1 = c0 + a.segs.nseg;
-  if (a.segs.off) {
+  if (a.segs.cu) {
+    const LaSpan x(a.segs, a.geo.T);
+    c0 = min(__builtin_amdgcn_readlane(x.first, s), a.segs.nslot);
+    c1 = min(__builtin_amdgcn_readlane(x.behind, s), a.segs.nslot);
+  } else if (a.segs.off) {
     c0 = min(max(ld_table(a.segs.off, s), 0), a.segs.nslot);
     c1 = min(max(ld_table(a.segs.off, s + 1), c0), a.segs.nslot);
   }
@@ -635,10 +675,11 @@ __global__ __launch_bounds__(256) void la_segcombine_kernel(LaScanArgs a, int si
     float d[AHEAD];
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
-      const int i = min(i0 + j, n - 1);
-      const size_t u = (size_t)(rev ? c1 - 1 - i : c0 + i) * H + h;
-      x[j] = *reinterpret_cast<const f4*>(N + u * size + e);
-      d[j] = a.dec[u];
+      if (i0 + j < n) {
+        const size_t u = (size_t)(rev ? c1 - 1 - (i0 + j) : c0 + i0 + j) * H + h;
+        x[j] = *reinterpret_cast<const f4*>(N + u * size + e);
+        d[j] = a.dec[u];
+      }
     }
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {

@@ -341,3 +341,15 @@ def test_refusals_launch_nothing():
     off = torch.zeros(4 * 2 * 64 + 1, dtype=torch.bfloat16, device="cuda")[1:].view(1, 4, 2, 64)
     with pytest.raises(g2.Gdr2Error):   # not 16-byte aligned
         g2.gdr2_linattn_fwd(off, h, h, torch.zeros((1, 4, 2), device="cuda"))
+
+
+@pytest.mark.parametrize("n", [63, 64, 65, 130])
+@pytest.mark.parametrize("at", [0, -1])
+def test_packed_many_sequences(n, at):
+    """Around the most sequences that a wave looks up by itself; a long one, of several segments, first or last."""
+    lengths = [(3 * i) % 7 for i in range(n)]
+    lengths[at] = 450
+    cu = np.concatenate([[0], np.cumsum(lengths)]).astype(int).tolist()
+    _case(f"packed {n} sequences, the long one at {at}")
+    d = _inputs(1, cu[-1], 1, 2, 64, 64, "bf16", "token", seed=n, n_seqs=n)
+    _check(d, "bf16", cu=cu, saved=n % 2 == 0)
