@@ -106,7 +106,7 @@ struct LaScanArgs {
   float *Pq, *Pk;        // grouped heads: dq, dk of each value head
   float *pa, *pb;        // q . dq and v . dv without the diagonal (rows, H)
   float *ca, *cb;        // sixteen parts of their chunk's sum of what comes from the state (slot, H, chunks a segment)
-  float *aS, *aD;        // S and dS at the anchors, (slot, H, anchors a segment)
+  float *aS, *aD;        // S and dS at the anchors inside segments, S at the last one's end (slot, H, anchors a segment)
   float* dg;             // (rows, H)
   int anchors;
 };

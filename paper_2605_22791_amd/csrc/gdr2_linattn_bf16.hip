@@ -832,7 +832,7 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
     const LaTab& t = tab[n & 1];
     const int cn = at(n);
     if constexpr (ROLE == kLaDv) {
-      if ((cn + 1) % kLaAnchor == 0 || n == 0)  // dS behind this chunk
+      if ((cn + 1) % kLaAnchor == 0 && n > 0)  // dS behind this chunk
         st.template store<B, TR>(a.aD + ((size_t)unit * a.anchors + cn / kLaAnchor) * (DK * DV), lane, wave);
     }
     f4 acc[2][4];
@@ -978,7 +978,7 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
     else
       st.template update<2>(sY, ax, z, REV ? t.E : t.T, lane);
     if constexpr (ROLE == kLaDq) {
-      if ((n + 1) % kLaAnchor == 0 || !more)
+      if (more ? (n + 1) % kLaAnchor == 0 : un.last && a.dST != nullptr)
         st.template store<B, TR>(a.aS + ((size_t)unit * a.anchors + n / kLaAnchor) * (DK * DV), lane, wave);
     }
     if (part)  // behind the tiles' loads lie the output's stores, at an anchor more
@@ -1043,8 +1043,13 @@ __global__ __launch_bounds__(kLaAnchor * CH) void la_dg_kernel(LaScanArgs a) {
     y = (double)a.ca[i] - a.cb[i];
   }
   double f = 0.0;
-  if (!(un.last && t0 + len == un.len && a.dST == nullptr)) {
-    const float *S = a.aS + (size_t)blockIdx.x * (DK * DV), *D = a.aD + (size_t)blockIdx.x * (DK * DV);
+  // S and dS behind the stretch: left by the scans, or behind the segment those that came before them
+  const bool end = t0 + len == un.len;
+  if (!(un.last && end && a.dST == nullptr)) {
+    const float* S = end && !un.last ? a.S + (size_t)unit * (DK * DV) : a.aS + (size_t)blockIdx.x * (DK * DV);
+    const float* D = !end      ? a.aD + (size_t)blockIdx.x * (DK * DV)
+                     : un.last ? a.dST + ((size_t)un.seq * H + h) * (DK * DV)
+                               : a.dS + ((size_t)unit + H) * (DK * DV);
     for (int e = 4 * tid; e < DK * DV; e += 4 * NTHR) {
       const float4 p = ld4(S + e), q = ld4(D + e);
       f += (double)(p.x * q.x + p.y * q.y) + (double)(p.z * q.z + p.w * q.w);
