@@ -23,17 +23,19 @@
 // What counts is how many instructions there are: a vector one takes 4 cycles of a SIMD's issue
 // and an MFMA 8 (of 16 that it is busy for) when waves share it, and at these rates the chip
 // draws its power: its clock falls to 1.6 GHz in the long scans, from 2.2 in short ones.
-// Two workgroups a CU (80 KB of LDS each) fill each other's gaps.
+// Two workgroups a CU (80 KB of LDS each) fill each other's gaps; the waves' priority (the scores,
+// short dependent steps that others wait for, over X St, that over the rest) keeps them in
+// different parts of a chunk: gradients 506 to 472 us, forward scan 144 to 130.
 //
 // Precision: inputs are exact bf16 operands.  fp32 operands are split: what only feeds bf16
 // outputs into two parts (16 bits, against the outputs' 8); the decayed Z of the update
 // (S_T, dS0 are fp32; of the forward's segments, in those that leave S_T), and the state and
 // scores where the decays' gradient reads the product, into three (24 bits).
 //
-// Measured, 8 x 4096 tokens, 16 heads of 128 x 128, four segments a sequence: forward scan 138 us
-// (537 MB, 3.9 TB/s), segment states 68 and 65 us, the three gradients 511 to 527 us (458 with
-// every load from the same place; 454 with two parts for three throughout, which costs the decays'
-// gradient its 1e-6), the decays' gradient 24 us.
+// Measured, 8 x 4096 tokens, 16 heads of 128 x 128, four segments a sequence: forward scan 130 us
+// (537 MB, 4.1 TB/s), segment states 68 and 65 us, the three gradients 472 us, the decays'
+// gradient 24 us.  Of 540 us before the priorities, every load from the same place took 458, two
+// parts for three throughout 454, at the cost of the decays' gradient's 1e-6.
 
 #include "gdr2_linattn.hpp"
 #include "gdr2_bf16.hpp"
@@ -825,6 +827,7 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
     }
   };
   for (int n = 0; n < nc; ++n) {
+    __builtin_amdgcn_s_setprio(1);
     __syncthreads();  // X and Z are there; Y, P and the terms of the chunk before are done with
     lx.load(Y, sx, lds + C::OFF_Y, wave);
     Y.next(sx);
@@ -847,6 +850,7 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
     la_zfrags(sZ, ax, z);
     la_landed<0>();
     __syncthreads();  // Y is there
+    __builtin_amdgcn_s_setprio(2);
     u4v er[SUMS ? 4 : 1];
     bf8 zr[SUMS ? 4 : 1];  // Z as the output lies
     if constexpr (SUMS) {
@@ -893,6 +897,7 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
       for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(er[i]));
     }
     __syncthreads();  // P is there; X and Z are done with
+    __builtin_amdgcn_s_setprio(0);
     if (more) {
       X.next(sx);
       Z.next(sz);
