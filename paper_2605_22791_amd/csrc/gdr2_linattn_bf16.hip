@@ -709,11 +709,15 @@ struct LaCfg {
   static_assert(LDS <= 80 * 1024, "two workgroups a CU");
 };
 
-template <int DK, int DV, int ROLE>
+// GROUPED: dq and dk of each value head leave in fp32, to be summed over their key head's.
+template <int DK, int DV, int ROLE, bool GROUPED>
 __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned char* smem) {
   using C = LaCfg<DK, DV, ROLE>;
   constexpr int A = C::A, B = C::B, NW = C::NW, TW = NW - 1, PARTS = C::PARTS;
   constexpr bool REV = C::REV, SUMS = C::SUMS, TR = C::TR;
+  constexpr bool PART = GROUPED && (ROLE == kLaDq || ROLE == kLaDk);
+  // The output's store instructions a chunk: for each block of 16 rows one of bf16, two of fp32 parts
+  constexpr int BLOCKS = CH / 16, STORES = PART ? 2 * BLOCKS : BLOCKS;
   const unsigned char *sX = smem, *sY = smem + C::OFF_Y, *sZ = smem + C::OFF_Z;
   __bf16* sP = reinterpret_cast<__bf16*>(smem + C::OFF_P);
   LaTab* tab = reinterpret_cast<LaTab*>(smem + C::OFF_T);
@@ -730,15 +734,14 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
   const size_t rk = (un.row0 * HK + hk) * DK, rv = (un.row0 * H + h) * DV;
   const bf16_t *q0 = a.q + rk, *k0 = a.k + rk, *v0 = a.v + rv, *d0 = a.dout + rv;
   // output: grouped heads' parts in fp32, a row for each value head, or bf16
-  float* part = ROLE == kLaDq ? a.Pq : ROLE == kLaDk ? a.Pk : nullptr;
-  const unsigned so = part ? 4u * H * DK : sz;
-  void* out0 = part ? (void*)(part + (un.row0 * H + h) * DK)
+  const unsigned so = PART ? 4u * H * DK : sz;
+  void* out0 = PART ? (void*)((ROLE == kLaDq ? a.Pq : a.Pk) + (un.row0 * H + h) * DK)
                     : (void*)(ROLE == kLaO ? a.o + rv : ROLE == kLaDv ? a.dv + rv : (ROLE == kLaDq ? a.dq : a.dk) + rk);
   LaRows<REV> X(ROLE == kLaO ? q0 : ROLE == kLaDq ? d0 : ROLE == kLaDv ? k0 : v0, sx, 2 * A, un.len);
   LaRows<REV> Y(ROLE == kLaO ? k0 : ROLE == kLaDq ? v0 : ROLE == kLaDv ? q0 : d0, sx, 2 * A, un.len);
   LaRows<REV> Z(ROLE == kLaO ? v0 : ROLE == kLaDq ? k0 : ROLE == kLaDv ? d0 : q0, sz, 2 * B, un.len);
   LaRows<REV> E(ROLE == kLaDq ? q0 : v0, sz, 2 * B, un.len);  // what the output is multiplied with for the decays' gradient
-  LaRows<REV> out(out0, so, part ? 4 * B : 2 * B, un.len);
+  LaRows<REV> out(out0, so, PART ? 4 * B : 2 * B, un.len);
   const float scale = a.geo.scale;
   const auto at = [&](int n) { return REV ? nc - 1 - n : n; };
   const auto rows = [&](int n) { return min(CH, un.len - CH * at(n)); };
@@ -785,8 +788,8 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
         *reinterpret_cast<bf4*>(sP + k * kLaScores + (REV ? la_ptile<REV>(3, 2) : la_ptile<REV>(2, 3)) * 256 + 4 * lane) = bf4{};
       }
     }
-    la_landed<0>();
   }
+  la_landed<0>();
   // chunk n's terms over the waves, a barrier after they were left
   const auto total = [&](int n) {
     float x = sA[lane] + sA[CH + lane];
@@ -935,11 +938,11 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
 #pragma unroll
             for (int k = 0; k < 2; ++k) acc[k][i] = mma(z[k][kb], p, acc[k][i]);
           }
-    float sum[SUMS ? 4 : 1];
+    float sum[SUMS ? BLOCKS : 1];
     const auto bo = out.buf();
     out.next(so);
 #pragma unroll
-    for (int i0 = 0; i0 < 4; i0 += 2) {
+    for (int i0 = 0; i0 < BLOCKS; i0 += 2) {
       if constexpr (SUMS) {
 #pragma unroll
         for (int i = i0; i < i0 + 2; ++i) {
@@ -955,7 +958,7 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
           }
         }
       }
-      if (part) {
+      if constexpr (PART) {
 #pragma unroll
         for (int i = i0; i < i0 + 2; ++i)
 #pragma unroll
@@ -986,10 +989,7 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
       if (more ? (n + 1) % kLaAnchor == 0 : un.last && a.dST != nullptr)
         st.template store<B, TR>(a.aS + ((size_t)unit * a.anchors + n / kLaAnchor) * (DK * DV), lane, wave);
     }
-    if (part)  // behind the tiles' loads lie the output's stores, at an anchor more
-      la_landed<16>();
-    else
-      la_landed<4>();
+    la_landed<STORES>();  // behind the tiles' loads lie the output's stores, at an anchor more
   }
   if constexpr (SUMS) {
     __syncthreads();
@@ -1006,20 +1006,20 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
 template <int DK, int DV>
 __global__ __launch_bounds__(2 * DV, 2) void la_scan_fwd_kernel(LaScanArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
-  la_scan<DK, DV, kLaO>(a, blockIdx.x, smem);
+  la_scan<DK, DV, kLaO, false>(a, blockIdx.x, smem);
 }
 // The gradients side by side.
-template <int DK, int DV>
+template <int DK, int DV, bool GROUPED>
 __global__ __launch_bounds__(2 * (DK > DV ? DK : DV), 2) void la_scan_bwd_kernel(LaScanArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
   int unit, role;
   if (!la_slot(blockIdx.x, a.segs.nslot * a.geo.H, unit, role)) return;
   if (role == kLaDq)
-    la_scan<DK, DV, kLaDq>(a, unit, smem);
+    la_scan<DK, DV, kLaDq, GROUPED>(a, unit, smem);
   else if (role == kLaDk)
-    la_scan<DK, DV, kLaDk>(a, unit, smem);
+    la_scan<DK, DV, kLaDk, GROUPED>(a, unit, smem);
   else
-    la_scan<DK, DV, kLaDv>(a, unit, smem);
+    la_scan<DK, DV, kLaDv, GROUPED>(a, unit, smem);
 }
 
 // ---- the decays' gradient --------------------------------------------------
@@ -1157,7 +1157,8 @@ hipError_t launch_la_scan_bwd(const LaScanArgs& a, hipStream_t st) {
   constexpr size_t lq = LaCfg<DK, DV, kLaDq>::LDS, lk = LaCfg<DK, DV, kLaDk>::LDS, lv = LaCfg<DK, DV, kLaDv>::LDS;
   constexpr size_t lds = lq > lk ? (lq > lv ? lq : lv) : (lk > lv ? lk : lv);
   const int units = a.segs.nslot * a.geo.H;
-  hipError_t e = la_launch(la_scan_bwd_kernel<DK, DV>, la_grid(units), 2 * (DK > DV ? DK : DV), lds, a, st);
+  const auto kernel = a.Pq ? la_scan_bwd_kernel<DK, DV, true> : la_scan_bwd_kernel<DK, DV, false>;
+  hipError_t e = la_launch(kernel, la_grid(units), 2 * (DK > DV ? DK : DV), lds, a, st);
   if (e == hipSuccess) {
     hipLaunchKernelGGL((la_dg_kernel<DK, DV>), dim3((unsigned)(units * a.anchors)), dim3(kLaAnchor * CH), 0, st, a);
     e = hipGetLastError();
