@@ -297,7 +297,9 @@ struct LaLoad {
 #pragma unroll
     for (int m = 0; m < NP; ++m) {
       const unsigned from = (off ^ (m & 1 ? 0x30 : 0)) + m * step, at = to + m * 1024;  // f(8) = 3
-      asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(from), "s"(buf) : "memory");
+      // m0, the place in LDS, has to be written a wait state before the load reads it
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(from), "s"(buf)
+                   : "memory", "m0");
     }
   }
 };

@@ -1,10 +1,13 @@
 """What the compiler cannot check of tile loads written out in assembly, on the built library's code.
 
 Linear attention's bf16 kernels load tiles from memory straight into LDS by instructions that the
-compiler does not count (la_landed waits for them).  Every path through every such kernel is walked here:
+compiler neither counts nor schedules (la_landed waits for them, LaLoad writes m0 before them).  Every
+path through every such kernel is walked here:
   * a wave meets a barrier only with its loads into LDS landed: the waves behind it read the tile.
     vmcnt(n) leaves the n youngest memory instructions in flight, so a load has landed if at least n
-    were issued behind it.
+    were issued behind it;
+  * a scalar write of m0, the loads' LDS address, is one wait state ahead of the load;
+  * scalar registers of the load's buffer come from vector instructions five wait states before.
 """
 
 import os
@@ -91,6 +94,17 @@ def _barriers_with_loads_under_way(code):
     return bad
 
 
+def _scalars(operands):
+    regs = set()
+    for a, b, c in re.findall(r"\bs\[(\d+):(\d+)\]|\bs(\d+)\b", operands):
+        regs |= set(range(int(a), int(b) + 1)) if a else {int(c)}
+    return regs
+
+
+def _states(ins):
+    return int(ins[2], 0) + 1 if ins[1] == "s_nop" else 1
+
+
 def test_kernels_that_load_into_lds_are_found(kernels):
     names = " ".join(kernels)
     assert all(n in names for n in ("la_segstate_kernel", "la_scan_fwd_kernel", "la_scan_bwd_kernel"))
@@ -99,6 +113,28 @@ def test_kernels_that_load_into_lds_are_found(kernels):
 def test_loads_into_lds_have_landed_at_barriers(kernels):
     bad = {n: [hex(a) for a in sorted(b)] for n, b in ((n, _barriers_with_loads_under_way(c)) for n, c in kernels.items()) if b}
     assert not bad, bad
+
+
+def test_m0_is_written_a_wait_state_before_a_load_into_lds(kernels):
+    bad = [(n, hex(ins[0])) for n, code in kernels.items() for before, ins in zip(code, code[1:])
+           if _to_lds(ins) and before[1].startswith("s_") and before[2].split(",")[0] == "m0"]
+    assert not bad, (len(bad), bad[:4])
+
+
+def test_buffers_of_loads_into_lds_are_not_fresh_from_vector_instructions(kernels):
+    bad = []
+    for n, code in kernels.items():
+        for i, ins in enumerate(code):
+            if not _to_lds(ins):
+                continue
+            need, ahead, j = _scalars(ins[2]), 0, i - 1
+            while j >= 0 and ahead < 5:
+                if code[j][1].startswith("v_") and need & _scalars(code[j][2].split(",")[0]):
+                    bad.append((n, hex(ins[0])))
+                    break
+                ahead += _states(code[j])
+                j -= 1
+    assert not bad, (len(bad), bad[:4])
 
 
 # ---- the walk itself, on a few lines -----------------------------------------
