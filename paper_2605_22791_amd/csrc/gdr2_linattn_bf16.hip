@@ -27,10 +27,11 @@
 // short dependent steps that others wait for, over X St, that over the rest) keeps them in
 // different parts of a chunk: gradients 506 to 472 us, forward scan 144 to 130.
 //
-// Precision: inputs are exact bf16 operands.  fp32 operands are split: what only feeds bf16
-// outputs into two parts (16 bits, against the outputs' 8); the decayed Z of the update
-// (S_T, dS0 are fp32; of the forward's segments, in those that leave S_T), and the state and
-// scores where the decays' gradient reads the product, into three (24 bits).
+// Precision: inputs are exact bf16 operands.  What is held in 32 bits between them, the state, the
+// scores and the decayed Z, enters the products split into three bf16 parts (24 bits, as many as it
+// has).  The decays' gradient and the fp32 states need them; o and dk, rounded to bf16 behind, would
+// pass their 2e-3 with two (16 bits), in 4 to 9 % less time, but then differ from the same rounding of
+// 32-bit values by 1e-4 of their norm, where three parts differ by 3e-5.
 //
 // Measured, 8 x 4096 tokens, 16 heads of 128 x 128, four segments a sequence: forward scan 130 us
 // (537 MB, 4.1 TB/s), segment states 68 and 65 us, the three gradients 472 us, the decays'
@@ -339,34 +340,32 @@ __device__ __forceinline__ void la_left(bf2 h, float& a, float& b) {
   a = __builtin_amdgcn_fdot2_f32_bf16(h, la_pick(0x0000bf80u), a, false);
   b = __builtin_amdgcn_fdot2_f32_bf16(h, la_pick(0xbf800000u), b, false);
 }
-template <int PARTS>
+constexpr int kLaParts = 3;
 struct LaFr {
-  bf8 p[PARTS];  // largest first
+  bf8 p[kLaParts];  // largest first
 };
-template <int PARTS>
-__device__ __forceinline__ LaFr<PARTS> la_split8(const float (&x)[8]) {
-  LaFr<PARTS> f;
+__device__ __forceinline__ LaFr la_split8(const float (&x)[8]) {
+  LaFr f;
 #pragma unroll
   for (int e = 0; e < 8; e += 2) {
     float a = x[e], b = x[e + 1];
 #pragma unroll
-    for (int k = 0; k < PARTS; ++k) {
+    for (int k = 0; k < kLaParts; ++k) {
       const bf2 h = la_part(a, b);
       f.p[k][e] = h[0];
       f.p[k][e + 1] = h[1];
-      if (k + 1 < PARTS) la_left(h, a, b);
+      if (k + 1 < kLaParts) la_left(h, a, b);
     }
   }
   return f;
 }
-template <int PARTS>
 __device__ __forceinline__ void la_split4(__bf16* p, int plane, const f4& x) {
   float r[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-  for (int k = 0; k < PARTS; ++k) {
+  for (int k = 0; k < kLaParts; ++k) {
     const bf2 h0 = la_part(r[0], r[1]), h1 = la_part(r[2], r[3]);
     *reinterpret_cast<bf4*>(p + k * plane) = bf4{h0[0], h0[1], h1[0], h1[1]};
-    if (k + 1 < PARTS) {
+    if (k + 1 < kLaParts) {
       la_left(h0, r[0], r[1]);
       la_left(h1, r[2], r[3]);
     }
@@ -441,8 +440,7 @@ struct LaState {
       }
   }
 
-  // acc[k][i] (elements 4 g + u of block k, row 16 i + c) = X St, the state split into PARTS; St <- eC St
-  template <int PARTS>
+  // acc[k][i] (elements 4 g + u of block k, row 16 i + c) = X St; St <- eC St
   __device__ __forceinline__ void read(const unsigned char* X, const LaAt& at, float eC, f4 (&acc)[2][4]) {
 #pragma unroll
     for (int k = 0; k < 2; ++k)
@@ -466,31 +464,30 @@ struct LaState {
 #pragma unroll
           for (int u = 0; u < 4; ++u) x[4 * e + u] = z[u];
         }
-        const LaFr<PARTS> f = la_split8<PARTS>(x);
+        const LaFr f = la_split8(x);
 #pragma unroll
-        for (int q = PARTS - 1; q >= 0; --q)
+        for (int q = kLaParts - 1; q >= 0; --q)
 #pragma unroll
           for (int i = 0; i < 4; ++i) acc[k][i] = mma(f.p[q], b[i], acc[k][i]);
       }
     }
   }
 
-  // St <- St + Y^T (w Z), w Z split into PARTS: z[k][kb] block k of the wave's Z columns, rows 32 kb + 8 g + e
-  template <int PARTS>
+  // St <- St + Y^T (w Z): z[k][kb] block k of the wave's Z columns, rows 32 kb + 8 g + e
   __device__ __forceinline__ void update(const unsigned char* Y, const LaAt& at, const bf8 (&z)[2][2], const float* w, int lane) {
     const int g = lane >> 4;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       float wv[8];
       ldf8(w + 32 * kb + 8 * g, wv);
-      LaFr<PARTS> d[2];
+      LaFr d[2];
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         float x[8];
         unpack8(z[k][kb], x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] *= wv[e];
-        d[k] = la_split8<PARTS>(x);
+        d[k] = la_split8(x);
       }
 #pragma unroll
       for (int t0 = 0; t0 < A / 16; t0 += 4) {
@@ -499,7 +496,7 @@ struct LaState {
 #pragma unroll
         for (int t = 0; t < 4; ++t) y[t] = la_ld_tr(yk + (at.tr[0] ^ (64 * (t >> 1))) + 8 * (t & 1), yk + (at.tr[1] ^ (64 * (t >> 1))) + 8 * (t & 1));
 #pragma unroll
-        for (int q = PARTS - 1; q >= 0; --q)
+        for (int q = kLaParts - 1; q >= 0; --q)
 #pragma unroll
           for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -643,7 +640,7 @@ __global__ __launch_bounds__(2 * DV, 2) void la_segstate_kernel(LaScanArgs a) {
     bf8 z[2][2];
     la_zfrags(sZ, ay, z);
     st.decay(t.eC);
-    st.template update<3>(sY, ay, z, REV ? t.E : t.T, lane);
+    st.update(sY, ay, z, REV ? t.E : t.T, lane);
   }
   float* N = (REV ? a.dS : a.S) + (size_t)unit * (DK * DV);
   st.template store<DV, false>(N, lane, wave);
@@ -703,9 +700,8 @@ struct LaCfg {
   static constexpr bool REV = ROLE == kLaDv || ROLE == kLaDk, TR = ROLE == kLaDq || ROLE == kLaDk;  // state transposed
   static constexpr bool SUMS = ROLE == kLaDq || ROLE == kLaDv;  // gives a term of the decays' gradient
   static constexpr int A = TR ? DV : DK, B = TR ? DK : DV, NW = B / 32;
-  static constexpr int PARTS = SUMS ? 3 : 2;  // of the state and the scores in products
   static constexpr int OFF_Y = la_bytes(A), OFF_Z = 2 * OFF_Y, OFF_P = OFF_Z + la_bytes(B);
-  static constexpr int OFF_S = OFF_P + PARTS * kLaScores * 2, OFF_T = OFF_S + NW * 2048;
+  static constexpr int OFF_S = OFF_P + kLaParts * kLaScores * 2, OFF_T = OFF_S + NW * 2048;
   static constexpr int OFF_A = OFF_T + 2 * (int)sizeof(LaTab);
   static constexpr int LDS = OFF_A + (SUMS ? (NW + 1) * CH * 4 + NW * 64 : 0);
   static_assert(LDS <= 80 * 1024, "two workgroups a CU");
@@ -715,7 +711,7 @@ struct LaCfg {
 template <int DK, int DV, int ROLE, bool GROUPED>
 __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned char* smem) {
   using C = LaCfg<DK, DV, ROLE>;
-  constexpr int A = C::A, B = C::B, NW = C::NW, TW = NW - 1, PARTS = C::PARTS;
+  constexpr int A = C::A, B = C::B, NW = C::NW, TW = NW - 1;
   constexpr bool REV = C::REV, SUMS = C::SUMS, TR = C::TR;
   constexpr bool PART = GROUPED && (ROLE == kLaDq || ROLE == kLaDk);
   // The output's store instructions a chunk: for each block of 16 rows one of bf16, two of fp32 parts
@@ -785,7 +781,7 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
     if (wave == TW) la_tables(g0, rows(0), tab[0], lane, scale);
     if (wave == 0) {  // the tiles past the diagonal
 #pragma unroll
-      for (int k = 0; k < PARTS; ++k) {
+      for (int k = 0; k < kLaParts; ++k) {
         *reinterpret_cast<bf4*>(sP + k * kLaScores + (REV ? la_ptile<REV>(1, 0) : la_ptile<REV>(0, 1)) * 256 + 4 * lane) = bf4{};
         *reinterpret_cast<bf4*>(sP + k * kLaScores + (REV ? la_ptile<REV>(3, 2) : la_ptile<REV>(2, 3)) * 256 + 4 * lane) = bf4{};
       }
@@ -803,9 +799,6 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
       (ROLE == kLaDq ? a.ca : a.cb)[((size_t)unit * (a.segs.seg_tokens / CH) + at(n)) * 16 + lane] = y;
     }
   };
-  // Parts of the decayed Z: two where the state feeds nothing but bf16 outputs (dk; o, but for
-  // the segment that leaves S_T: the states between segments come of their own pass)
-  const bool exact = SUMS || (ROLE == kLaO && un.last && a.ST != nullptr);
   const auto scores = [&](auto count, auto diag, int n0, const LaTab& t) {
     constexpr int N = decltype(count)::value;
     constexpr bool DIAG = decltype(diag)::value;
@@ -828,7 +821,7 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
 #pragma unroll
         for (int u = 0; u < 4; ++u) x[m][u] = u == u0 ? 0.f : x[m][u];
       }
-      la_split4<PARTS>(sP + la_ptile<REV>(io[m], jz[m]) * 256 + 16 * c + 4 * g, kLaScores, x[m]);
+      la_split4(sP + la_ptile<REV>(io[m], jz[m]) * 256 + 16 * c + 4 * g, kLaScores, x[m]);
     }
   };
   for (int n = 0; n < nc; ++n) {
@@ -844,7 +837,7 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
         st.template store<B, TR>(a.aD + ((size_t)unit * a.anchors + cn / kLaAnchor) * (DK * DV), lane, wave);
     }
     f4 acc[2][4];
-    st.template read<PARTS>(sX, ax, t.eC, acc);
+    st.read(sX, ax, t.eC, acc);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float f = (REV ? t.T : t.E)[16 * i + c];
@@ -930,7 +923,7 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
     }
     const __bf16* pf = sP + 256 * (g >> 1) + 16 * c + 8 * (g & 1);
 #pragma unroll
-    for (int q = PARTS - 1; q >= 0; --q)
+    for (int q = kLaParts - 1; q >= 0; --q)
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -983,10 +976,7 @@ __device__ __forceinline__ void la_scan(const LaScanArgs& a, int unit, unsigned 
       }
     }
     if constexpr (SUMS) sA[wave * CH + lane] = la_sum4(sum);
-    if (exact)
-      st.template update<3>(sY, ax, z, REV ? t.E : t.T, lane);
-    else
-      st.template update<2>(sY, ax, z, REV ? t.E : t.T, lane);
+    st.update(sY, ax, z, REV ? t.E : t.T, lane);
     if constexpr (ROLE == kLaDq) {
       if (more ? (n + 1) % kLaAnchor == 0 : un.last && a.dST != nullptr)
         st.template store<B, TR>(a.aS + ((size_t)unit * a.anchors + n / kLaAnchor) * (DK * DV), lane, wave);
