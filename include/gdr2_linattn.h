@@ -24,7 +24,11 @@
  * are overwritten.  An empty sequence of a packed batch passes S0 to S_T and dS_T to dS0.
  *
  * A non-finite value in a token's q, k, v or dout reaches the outputs of its own
- * 64-token chunk on both sides of the token, and what follows from the state.
+ * 64-token chunk on both sides of the token, and what follows from the state: the tokens
+ * behind the chunk and S_T from k and v, those before it and dS0 from q and dout.  In bf16
+ * problems one in k or v also reaches dg of up to 1023 tokens before it, for the decays'
+ * gradient is summed backwards over stretches of 1024 tokens from the state behind them.
+ * With GDR2_DECAY_HEAD, dg of a head is a sum over all of these.
  */
 #ifndef GDR2_LINATTN_H_
 #define GDR2_LINATTN_H_
