@@ -22,6 +22,12 @@ sys.path.insert(0, os.path.join(os.path.dirname(os.path.abspath(__file__)), ".."
 import paper_2605_22791_amd as g2  # noqa: E402
 
 
+def once():
+    """Of a backward: the kernels' results carry no graph, so under create_graph=True terms would be left out silently."""
+    if torch.is_grad_enabled():
+        raise RuntimeError("the operators have no second derivative: create_graph=True is not supported")
+
+
 class Attention(torch.autograd.Function):
     """o, S_T of linear attention; the workspace takes the forward's states to the backward."""
 
@@ -37,6 +43,7 @@ class Attention(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, do, dS):
+        once()
         q, k, v, g, S0, ws = ctx.saved_tensors
         d = g2.gdr2_linattn_bwd(q, k, v, g, S0, do.contiguous(), dS.contiguous(), want_dS0=S0 is not None, ws=ws,
                                 saved=True)
@@ -54,6 +61,7 @@ class BlockNorm(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dh, dn):
+        once()
         y, w_post, gate, x, res_scale, w_pre = ctx.saved_tensors
         d = g2.gdr2_blocknorm_bwd(y, dh.contiguous(), None if w_pre is None else dn.contiguous(), w_post=w_post, gate=gate,
                                   x=x, res_scale=res_scale, w_pre=w_pre)

@@ -61,3 +61,16 @@ def test_gradients_follow_differences(example):
         b = loss()
     fall = (float(a.detach()) - float(b)) / (step * size)
     assert 0.5 < fall < 1.5, fall
+
+
+def test_a_second_derivative_is_refused(example):
+    """A penalty on a gradient raises instead of leaving out what goes through the operators."""
+    print("second derivatives", flush=True)
+    q, k, v, z = (torch.randn(1, 20, 2, 64, device="cuda").to(torch.bfloat16).requires_grad_(True) for _ in range(4))
+    w = torch.ones(64, device="cuda", requires_grad=True)
+    o, _ = example.Attention.apply(q, k, v, -torch.rand(1, 20, 2, device="cuda"), None)
+    a, _ = example.BlockNorm.apply(v, w, z, None, None, None)
+    for y, x in ((o, q), (a, v)):
+        with pytest.raises(RuntimeError, match="second derivative"):
+            d, = torch.autograd.grad(y.float().sum(), x, create_graph=True)
+            (x.float() ** 2 + d.float() ** 2).sum().backward()
