@@ -41,29 +41,27 @@ __device__ __forceinline__ float la_decay_at(const LaGeo& a, size_t row, int h) 
   return g < kLaForget ? kLaForget : g;
 }
 
-template <typename TIn>
+// ---- fp32 problems: chunk-parallel passes ----------------------------------
 struct LaFwdArgs {
   LaGeo geo;
-  const TIn *q, *k, *v;
-  TIn* o;
-  const float *S0, *N, *eGC;  // chunk-start states, exp(G_C)
+  const float *q, *k, *v;
+  float* o;
+  const float* N;  // states that enter the chunks
 };
 
-template <typename TIn>
 struct LaBwdArgs {
   LaGeo geo;
-  const TIn *q, *k, *v, *dout;
-  TIn *dq, *dk, *dv;
+  const float *q, *k, *v, *dout;
+  float *dq, *dk, *dv;
   float *Pq, *Pk;  // grouped heads: dq, dk of each value head (rows, H, Dk), else null
   float* dg;       // (rows, H)
-  const float *N, *M, *eGC;
+  const float *N, *M;  // as above, and the gradients of the states behind them
 };
 
 // N_n = sum_s w_s x_s z_s^T of every chunk, w_s = exp(G_C - G_s), or scale exp(G_s) (rev)
-template <typename TIn>
 struct LaStateArgs {
   LaGeo geo;
-  const TIn *x, *z;
+  const float *x, *z;
   float *N, *eGC;
 };
 
@@ -131,13 +129,13 @@ struct LaStepArgs {
   float scale;
 };
 
-template <int DK, int DV, typename TIn>
-hipError_t launch_la_state(const LaStateArgs<TIn>& fwd, const LaStateArgs<TIn>& rev, hipStream_t st);  // of N null: none
+template <int DK, int DV>
+hipError_t launch_la_state(const LaStateArgs& fwd, const LaStateArgs& rev, hipStream_t st);  // of N null: none
 hipError_t launch_la_combine(const LaCombineArgs& fwd, const LaCombineArgs& rev, hipStream_t st);  // of N null: none
-template <int DK, int DV, typename TIn>
-hipError_t launch_la_fwd(const LaFwdArgs<TIn>& a, hipStream_t st);
-template <int DK, int DV, typename TIn>
-hipError_t launch_la_bwd(const LaBwdArgs<TIn>& a, hipStream_t st);
+template <int DK, int DV>
+hipError_t launch_la_fwd(const LaFwdArgs& a, hipStream_t st);
+template <int DK, int DV>
+hipError_t launch_la_bwd(const LaBwdArgs& a, hipStream_t st);
 template <int DK, int DV, typename TIn>
 hipError_t launch_la_step(const LaStepArgs<TIn>& a, hipStream_t st);
 // out[r][h][c] = sum over the group's value heads of P[r][h G + j][c]

@@ -147,10 +147,10 @@ hipError_t la_table(const gdr2_problem* p, const LaLayout& L, const int32_t* cu,
 
 // the states that enter the chunks, from k and v, and the gradients of their end states, from q and
 // dout: those of them whose N is given
-template <int DK, int DV, typename TIn>
-hipError_t la_states(const LaStateArgs<TIn>& fwd, const LaStateArgs<TIn>& rev, const LaCombineArgs& cf,
-                     const LaCombineArgs& cr, hipStream_t st) {
-  const hipError_t e = launch_la_state<DK, DV, TIn>(fwd, rev, st);
+template <int DK, int DV>
+hipError_t la_states(const LaStateArgs& fwd, const LaStateArgs& rev, const LaCombineArgs& cf, const LaCombineArgs& cr,
+                     hipStream_t st) {
+  const hipError_t e = launch_la_state<DK, DV>(fwd, rev, st);
   return e != hipSuccess ? e : launch_la_combine(cf, cr, st);
 }
 
@@ -196,11 +196,11 @@ hipError_t la_fwd(const gdr2_problem* p, const LaLayout& L, const LaGeo& geo, co
     return e != hipSuccess ? e : launch_la_scan_fwd<DK, DV>(a, st);
   } else {
     float *N = at<float>(ws, L.N), *eGC = at<float>(ws, L.eGC);
-    hipError_t e = la_states<DK, DV, TIn>({geo, static_cast<const TIn*>(k), static_cast<const TIn*>(v), N, eGC}, {},
-                                          {geo, N, eGC, S0, ST, nseq > 0 ? nseq : p->B, DK * DV, 0}, {}, st);
+    hipError_t e = la_states<DK, DV>({geo, static_cast<const float*>(k), static_cast<const float*>(v), N, eGC}, {},
+                                     {geo, N, eGC, S0, ST, nseq > 0 ? nseq : p->B, DK * DV, 0}, {}, st);
     if (e != hipSuccess) return e;
-    return launch_la_fwd<DK, DV, TIn>({geo, static_cast<const TIn*>(q), static_cast<const TIn*>(k),
-                                       static_cast<const TIn*>(v), static_cast<TIn*>(o), S0, N, eGC}, st);
+    return launch_la_fwd<DK, DV>({geo, static_cast<const float*>(q), static_cast<const float*>(k),
+                                  static_cast<const float*>(v), static_cast<float*>(o), N}, st);
   }
 }
 
@@ -240,18 +240,18 @@ hipError_t la_bwd(const gdr2_problem* p, const LaLayout& L, const LaGeo& geo, co
   } else {
     const int ns = nseq > 0 ? nseq : p->B;
     float *N = at<float>(ws, L.N), *M = at<float>(ws, L.M), *eGC = at<float>(ws, L.eGC);
-    LaStateArgs<TIn> fwd{};
+    LaStateArgs fwd{};
     LaCombineArgs cf{};
     if (!saved) {
-      fwd = {geo, static_cast<const TIn*>(k), static_cast<const TIn*>(v), N, eGC};
+      fwd = {geo, static_cast<const float*>(k), static_cast<const float*>(v), N, eGC};
       cf = {geo, N, eGC, S0, nullptr, ns, DK * DV, 0};
     }
-    e = la_states<DK, DV, TIn>(fwd, {geo, static_cast<const TIn*>(q), static_cast<const TIn*>(dout), M, eGC}, cf,
-                               {geo, M, eGC, dST, d.dS0, ns, DK * DV, 1}, st);
+    e = la_states<DK, DV>(fwd, {geo, static_cast<const float*>(q), static_cast<const float*>(dout), M, eGC}, cf,
+                          {geo, M, eGC, dST, d.dS0, ns, DK * DV, 1}, st);
     if (e != hipSuccess) return e;
-    e = launch_la_bwd<DK, DV, TIn>({geo, static_cast<const TIn*>(q), static_cast<const TIn*>(k),
-                                    static_cast<const TIn*>(v), static_cast<const TIn*>(dout), static_cast<TIn*>(d.dq),
-                                    static_cast<TIn*>(d.dk), static_cast<TIn*>(d.dv), Pq, Pk, dg, N, M, eGC}, st);
+    e = launch_la_bwd<DK, DV>({geo, static_cast<const float*>(q), static_cast<const float*>(k),
+                               static_cast<const float*>(v), static_cast<const float*>(dout), static_cast<float*>(d.dq),
+                               static_cast<float*>(d.dk), static_cast<float*>(d.dv), Pq, Pk, dg, N, M}, st);
   }
   if (e == hipSuccess && geo.G > 1)
     e = launch_la_group<TIn>(Pq, Pk, static_cast<TIn*>(d.dq), static_cast<TIn*>(d.dk), rows, geo.H / geo.G, geo.G, DK, st);

@@ -23,10 +23,6 @@ constexpr int kThr = 256;
 // with eight and sixteen 12.5, 18.6, 49.
 constexpr int kThrState = 512, kThrRows = 1024;
 
-__device__ __forceinline__ void la_load4(const float* p, float (&x)[4]) {
-  const float4 t = ld4(p);
-  x[0] = t.x, x[1] = t.y, x[2] = t.z, x[3] = t.w;
-}
 __device__ __forceinline__ void la_put(float* p, float x) { *p = x; }
 __device__ __forceinline__ void la_put(bf16_t* p, float x) {
   *reinterpret_cast<__bf16*>(p) = (__bf16)x;
@@ -55,13 +51,12 @@ __device__ __forceinline__ void la_sums(const LaGeo& a, const ChunkPos& p, int h
 __device__ __forceinline__ float la_exp(double x) { return expf((float)x); }
 
 // 64 x D tile of one head into LDS as fp32 (row stride D + 4), rows >= len zero.
-template <int D, int NTHR, typename TIn>
-__device__ __forceinline__ void la_tile(const TIn* src, size_t stride, int len, float* dst, int tid) {
+template <int D, int NTHR>
+__device__ __forceinline__ void la_tile(const float* src, size_t stride, int len, float* dst, int tid) {
   for (int e = tid; e < CH * D / 4; e += NTHR) {
     const int r = e / (D / 4), c = (e % (D / 4)) * 4;
-    float x[4] = {0.f, 0.f, 0.f, 0.f};
-    if (r < len) la_load4(src + r * stride + c, x);
-    *reinterpret_cast<float4*>(dst + r * (D + 4) + c) = make_float4(x[0], x[1], x[2], x[3]);
+    const float4 x = r < len ? ld4(src + r * stride + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+    *reinterpret_cast<float4*>(dst + r * (D + 4) + c) = x;
   }
 }
 
@@ -141,8 +136,8 @@ __device__ __forceinline__ f4 la_cols_tile(const float* P, const float* Z, int j
 }  // namespace
 
 // ---- every chunk's contribution to the state -------------------------------
-template <int DK, int DV, typename TIn, bool REV>
-__device__ __forceinline__ void la_state(const LaStateArgs<TIn>& a, float* smem) {
+template <int DK, int DV, bool REV>
+__device__ __forceinline__ void la_state(const LaStateArgs& a, float* smem) {
   __shared__ double sG[CH + 1];
   __shared__ float sW[CH];
   float *sX = smem, *sZ = sX + CH * (DK + 4);
@@ -178,13 +173,13 @@ __device__ __forceinline__ void la_state(const LaStateArgs<TIn>& a, float* smem)
 }
 
 // Of the states, their gradients, or (grid y) the two side by side.
-template <int DK, int DV, typename TIn>
-__global__ __launch_bounds__(kThrState) void la_state_kernel(LaStateArgs<TIn> fwd, LaStateArgs<TIn> rev) {
+template <int DK, int DV>
+__global__ __launch_bounds__(kThrState) void la_state_kernel(LaStateArgs fwd, LaStateArgs rev) {
   extern __shared__ __align__(16) float smem[];
   if (blockIdx.y == 0 && fwd.N)
-    la_state<DK, DV, TIn, false>(fwd, smem);
+    la_state<DK, DV, false>(fwd, smem);
   else
-    la_state<DK, DV, TIn, true>(rev, smem);
+    la_state<DK, DV, true>(rev, smem);
 }
 
 // ---- the states that enter the chunks --------------------------------------
@@ -225,8 +220,8 @@ __global__ __launch_bounds__(kThr) void la_combine_kernel(LaCombineArgs fwd, LaC
 
 // ---- outputs ---------------------------------------------------------------
 // wave 4 m + i: rows 16 i .., every fourth block of columns from m on
-template <int DK, int DV, typename TIn>
-__global__ __launch_bounds__(kThrRows) void la_fwd_kernel(LaFwdArgs<TIn> a) {
+template <int DK, int DV>
+__global__ __launch_bounds__(kThrRows) void la_fwd_kernel(LaFwdArgs a) {
   __shared__ double sG[CH + 1];
   extern __shared__ __align__(16) float smem[];
   float *sQ = smem, *sK = sQ + CH * (DK + 4), *sV = sK + CH * (DK + 4), *sP = sV + CH * (DV + 4);
@@ -253,7 +248,7 @@ __global__ __launch_bounds__(kThrRows) void la_fwd_kernel(LaFwdArgs<TIn> a) {
 #pragma unroll
   for (int u = 0; u < 4; ++u) er[u] = la_exp(sG[16 * i + 4 * g + u + 1]);
   const float* S = a.N + p.ch * (size_t)(DK * DV);
-  TIn* o = a.o + (p.row0 * H + h) * DV;
+  float* o = a.o + (p.row0 * H + h) * DV;
   for (int t = m; t < DV / 16; t += kThrRows / 256) {
     f4 acc = la_state_tile<DK, DV>(sQ, S, 16 * i, 16 * t, f4{0.f, 0.f, 0.f, 0.f}, lane);
 #pragma unroll
@@ -262,15 +257,15 @@ __global__ __launch_bounds__(kThrRows) void la_fwd_kernel(LaFwdArgs<TIn> a) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int r = 16 * i + 4 * g + u;
-      if (r < p.len) la_put(o + (size_t)r * H * DV + 16 * t + l, a.geo.scale * acc[u]);
+      if (r < p.len) o[(size_t)r * H * DV + 16 * t + l] = a.geo.scale * acc[u];
     }
   }
 }
 
 // ---- gradients -------------------------------------------------------------
 // waves as above
-template <int DK, int DV, typename TIn>
-__global__ __launch_bounds__(kThrRows) void la_bwd_kernel(LaBwdArgs<TIn> a) {
+template <int DK, int DV>
+__global__ __launch_bounds__(kThrRows) void la_bwd_kernel(LaBwdArgs a) {
   __shared__ double sG[CH + 1];
   constexpr int NM = kThrRows / 256;
   __shared__ float sA[NM][CH], sB[NM][CH], sRow[NM][CH], sCol[4][CH], sE[kThrRows / 64];
@@ -346,7 +341,7 @@ __global__ __launch_bounds__(kThrRows) void la_bwd_kernel(LaBwdArgs<TIn> a) {
       const int r = 16 * i + 4 * g + u;
       inter[u] *= tail[u];
       dot[u] += inter[u] * sV[r * (DV + 4) + 16 * t + l];
-      if (r < p.len) la_put(a.dv + ((p.row0 + r) * H + h) * DV + 16 * t + l, inter[u] + scale * intra[u]);
+      if (r < p.len) a.dv[((p.row0 + r) * H + h) * DV + 16 * t + l] = inter[u] + scale * intra[u];
     }
   }
 #pragma unroll
@@ -379,8 +374,8 @@ __global__ __launch_bounds__(kThrRows) void la_bwd_kernel(LaBwdArgs<TIn> a) {
           a.Pk[at] = dk;
         } else {
           const size_t at = ((p.row0 + r) * HK + hk) * DK + 16 * t + l;
-          la_put(a.dq + at, dq);
-          la_put(a.dk + at, dk);
+          a.dq[at] = dq;
+          a.dk[at] = dk;
         }
       }
     }
@@ -450,12 +445,12 @@ hipError_t la_lds(K kernel, size_t bytes) {
 }
 }  // namespace
 
-template <int DK, int DV, typename TIn>
-hipError_t launch_la_state(const LaStateArgs<TIn>& fwd, const LaStateArgs<TIn>& rev, hipStream_t st) {
+template <int DK, int DV>
+hipError_t launch_la_state(const LaStateArgs& fwd, const LaStateArgs& rev, hipStream_t st) {
   constexpr size_t lds = 4 * CH * (DK + DV + 8);
-  hipError_t e = la_lds(la_state_kernel<DK, DV, TIn>, lds);
+  hipError_t e = la_lds(la_state_kernel<DK, DV>, lds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((la_state_kernel<DK, DV, TIn>), dim3(la_units((fwd.N ? fwd : rev).geo), fwd.N && rev.N ? 2 : 1),
+  hipLaunchKernelGGL((la_state_kernel<DK, DV>), dim3(la_units((fwd.N ? fwd : rev).geo), fwd.N && rev.N ? 2 : 1),
                      dim3(kThrState), lds, st, fwd, rev);
   return hipGetLastError();
 }
@@ -467,21 +462,21 @@ hipError_t launch_la_combine(const LaCombineArgs& fwd, const LaCombineArgs& rev,
   return hipGetLastError();
 }
 
-template <int DK, int DV, typename TIn>
-hipError_t launch_la_fwd(const LaFwdArgs<TIn>& a, hipStream_t st) {
+template <int DK, int DV>
+hipError_t launch_la_fwd(const LaFwdArgs& a, hipStream_t st) {
   constexpr size_t lds = 4 * CH * (2 * (DK + 4) + DV + 4 + LP);
-  hipError_t e = la_lds(la_fwd_kernel<DK, DV, TIn>, lds);
+  hipError_t e = la_lds(la_fwd_kernel<DK, DV>, lds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((la_fwd_kernel<DK, DV, TIn>), dim3(la_units(a.geo)), dim3(kThrRows), lds, st, a);
+  hipLaunchKernelGGL((la_fwd_kernel<DK, DV>), dim3(la_units(a.geo)), dim3(kThrRows), lds, st, a);
   return hipGetLastError();
 }
 
-template <int DK, int DV, typename TIn>
-hipError_t launch_la_bwd(const LaBwdArgs<TIn>& a, hipStream_t st) {
+template <int DK, int DV>
+hipError_t launch_la_bwd(const LaBwdArgs& a, hipStream_t st) {
   constexpr size_t lds = 4 * CH * (2 * (DK + 4) + 2 * (DV + 4) + LP);
-  hipError_t e = la_lds(la_bwd_kernel<DK, DV, TIn>, lds);
+  hipError_t e = la_lds(la_bwd_kernel<DK, DV>, lds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((la_bwd_kernel<DK, DV, TIn>), dim3(la_units(a.geo)), dim3(kThrRows), lds, st, a);
+  hipLaunchKernelGGL((la_bwd_kernel<DK, DV>), dim3(la_units(a.geo)), dim3(kThrRows), lds, st, a);
   return hipGetLastError();
 }
 
@@ -500,12 +495,13 @@ hipError_t launch_la_headsum(const float* P, float* dg, size_t rows, int H, hipS
   return hipGetLastError();
 }
 
-#define GDR2_LA_INST(DK, DV, T)                                                                   \
-  template hipError_t launch_la_state<DK, DV, T>(const LaStateArgs<T>&, const LaStateArgs<T>&, hipStream_t); \
-  template hipError_t launch_la_fwd<DK, DV, T>(const LaFwdArgs<T>&, hipStream_t);                 \
-  template hipError_t launch_la_bwd<DK, DV, T>(const LaBwdArgs<T>&, hipStream_t);
-#define GDR2_LA_INST4(T) \
-  GDR2_LA_INST(64, 64, T) GDR2_LA_INST(64, 128, T) GDR2_LA_INST(128, 64, T) GDR2_LA_INST(128, 128, T)
-GDR2_LA_INST4(float)
+#define GDR2_LA_INST(DK, DV)                                                                   \
+  template hipError_t launch_la_state<DK, DV>(const LaStateArgs&, const LaStateArgs&, hipStream_t); \
+  template hipError_t launch_la_fwd<DK, DV>(const LaFwdArgs&, hipStream_t);                    \
+  template hipError_t launch_la_bwd<DK, DV>(const LaBwdArgs&, hipStream_t);
+GDR2_LA_INST(64, 64)
+GDR2_LA_INST(64, 128)
+GDR2_LA_INST(128, 64)
+GDR2_LA_INST(128, 128)
 
 }  // namespace gdr2
