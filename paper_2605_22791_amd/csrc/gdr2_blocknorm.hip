@@ -16,6 +16,10 @@
 // TB/s), backward 134 us (671 MB, 5.0 TB/s; 212 without the row ahead and in the
 // registers of the full form); 32768 rows of 2048, everything, fp32 stream: 166 us
 // (0.94 GB) and 336 us (1.47 GB, 4.4 TB/s); 1999 fp32 rows of 1155: 11 and 19 us.
+// Far from that: the backward of rows over 4096 with stream parts, whose 1024 lanes of 128
+// registers spill (8192 rows of 8192: 1340 us for 1.47 GB), and widths that 8 does not divide in
+// bf16, loaded two bytes at a time (58099 rows of 1155, everything: 333 and 1171 us for the
+// same bytes).
 
 #include "gdr2_blocknorm.hpp"
 #include "gdr2_bf16.hpp"

@@ -80,8 +80,8 @@ struct LaCombineArgs {
 // sequence has one without tokens); slot = sequence * nseg + segment, or, packed, an
 // entry of a table: first token, tokens and sequence of every slot, and the first
 // slot of every sequence.  Up to 64 sequences need no table: a wave looks a slot up in
-// the offsets, a sequence a lane (nine prompts of 8192 tokens in all: 75 us a
-// forward call, 77 with the launch that writes the table and the reads of it).
+// the offsets, a sequence a lane (nine prompts of 8192 tokens in all: 84 us a
+// forward call, 87 with the launch that writes the table and the reads of it).
 struct LaSegs {
   const int *t0 = nullptr, *len = nullptr, *seq = nullptr, *off = nullptr;  // packed only
   const int* cu = nullptr;  // packed, up to 64 sequences: in place of the table

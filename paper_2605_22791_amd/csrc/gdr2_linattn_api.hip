@@ -32,11 +32,12 @@ struct LaLayout {
 };
 
 // Tokens of a segment.  A workgroup scans one head's segment, two are on a CU at a time: sequences
-// are cut into as many as fill the 256 CUs once.  (Twice as many, in two rounds, took 89 us where
-// one round took 81, nine packed prompts of 8192 tokens in all, 16 value heads: each segment
-// costs its state's way to memory and back.)  A packed batch counts as one sequence of its total
-// length, beside a slot for the end of each, for its lengths are on the device.  Cutting takes two
-// more launches: up to three chunks (T 192, 16 heads: 15.2 us whole, 17.1 cut) are left whole.
+// are cut into as many as fill the 256 CUs once.  (Twice as many, in two rounds, took 95 us where
+// one round took 84, nine packed prompts of 8192 tokens in all, 16 value heads, and 809 where one
+// took 738, training at 8 x 4096 tokens: each segment costs its state's way to memory and back.)
+// A packed batch counts as one sequence of its total length, beside a slot for the end of each, for
+// its lengths are on the device.  Cutting takes two more launches: up to three chunks (T 192, 16
+// heads: 18 us a call whole, 24 cut) are left whole.
 int la_seg_tokens(const gdr2_problem* p, int nseq) {
   const int NT = chunks_per_seq(p);
   const long long H = value_view(p).H, base = (nseq > 0 ? 1 : p->B) * H;

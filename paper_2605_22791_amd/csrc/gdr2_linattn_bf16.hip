@@ -25,7 +25,7 @@
 // draws its power: its clock falls to 1.6 GHz in the long scans, from 2.2 in short ones.
 // Two workgroups a CU (80 KB of LDS each) fill each other's gaps; the waves' priority (the scores,
 // short dependent steps that others wait for, over X St, that over the rest) keeps them in
-// different parts of a chunk: gradients 506 to 472 us, forward scan 144 to 130.
+// different parts of a chunk: gradients 552 to 518 us, forward scan 164 to 148.
 //
 // Precision: inputs are exact bf16 operands.  What is held in 32 bits between them, the state, the
 // scores and the decayed Z, enters the products split into three bf16 parts (24 bits, as many as it
@@ -33,10 +33,11 @@
 // pass their 2e-3 with two (16 bits), in 4 to 9 % less time, but then differ from the same rounding of
 // 32-bit values by 1e-4 of their norm, where three parts differ by 3e-5.
 //
-// Measured, 8 x 4096 tokens, 16 heads of 128 x 128, four segments a sequence: forward scan 130 us
-// (537 MB, 4.1 TB/s), segment states 68 and 65 us, the three gradients 472 us, the decays'
-// gradient 24 us.  Of 540 us before the priorities, every load from the same place took 458, two
-// parts for three throughout 454, at the cost of the decays' gradient's 1e-6.
+// Measured, 8 x 4096 tokens, 16 heads of 128 x 128, four segments a sequence: forward scan 148 us
+// (537 MB, 3.6 TB/s), segment states 70 and 67 us, the three gradients 518 us (2 GB read and
+// written, 3.8 TB/s), the decays' gradient 24 us.  Of the gradients' 518 us, tiles all from the same
+// place take 485 and two parts for three 414: it is the instructions of the split products, and the
+// power they draw, rather than memory.
 
 #include "gdr2_linattn.hpp"
 #include "gdr2_bf16.hpp"
@@ -115,7 +116,8 @@ __device__ __forceinline__ bool la_unit(const LaSegs& s, int T, int slot, LaUnit
 
 // Workgroup b of the gradients' grid: first dq and dv, the longer ones, of eight units after each
 // other, then dk.  Blocks go to the eight XCDs in turn, so a unit's run on one and share its L2.
-// (All three of a unit together took 543 us for 521 at 8 x 4096 tokens, 16 heads: a tail of long ones.)
+// (A training step with all three of a unit together: 1 % less at 8 x 4096 tokens, 16 heads of
+// 128 x 128, but 2 % more there at 64 x 64 and in packed batches, 5 % more at 128 x 64: a tail of long ones.)
 __device__ __forceinline__ bool la_slot(int b, int n, int& unit, int& role) {
   const int n8 = (n + 7) / 8 * 8;
   if (b < 2 * n8) {
