@@ -6,8 +6,11 @@ shapes and dtypes are read from the torch tensors, outputs and workspace are
 allocated with torch when the caller does not pass them, and every step of the
 operator runs in the HIP kernels of the library on the current torch stream.
 
-Linear attention with a decay for each head (linattn.py, include/gdr2_linattn.h)
-and the block norms (blocknorm.py, include/gdr2_blocknorm.h) are called the same way.
+Linear attention with a decay for each head (linattn.py, include/gdr2_linattn.h), the
+block norms (blocknorm.py, include/gdr2_blocknorm.h), the gated linear recurrence
+(gatedrec.py, include/gdr2_gatedrec.h), the gated feed-forward block (gatedff.py,
+include/gdr2_gatedff.h) and dropout with the residual sum (dropout.py,
+include/gdr2_dropout.h) are called the same way.
 
 If the library is missing the functions raise; there is no fallback.
 """
@@ -114,6 +117,9 @@ def lib():
         L.gdr2_status_str.restype = ctypes.c_char_p
         linattn._declare(L)
         blocknorm._declare(L)
+        gatedrec._declare(L)
+        gatedff._declare(L)
+        dropout._declare(L)
         _LIB = L
     return _LIB
 
@@ -568,8 +574,11 @@ def gdr2_fused_recurrent(q, k, v, f, a_log, delta, b, w, S, *, cu_seqlens=None, 
 
 
 # --------------------------------------------------------------------------- the other operators
-from . import linattn, blocknorm  # noqa: E402  (they use the helpers above)
+from . import linattn, blocknorm, gatedrec, gatedff, dropout  # noqa: E402  (they use the helpers above)
 from .linattn import *  # noqa: E402,F401,F403
 from .blocknorm import *  # noqa: E402,F401,F403
+from .gatedrec import *  # noqa: E402,F401,F403
+from .gatedff import *  # noqa: E402,F401,F403
+from .dropout import *  # noqa: E402,F401,F403
 
-__all__ += linattn.__all__ + blocknorm.__all__
+__all__ += linattn.__all__ + blocknorm.__all__ + gatedrec.__all__ + gatedff.__all__ + dropout.__all__
