@@ -8,10 +8,10 @@
 // registers, a lane one or two channels.  A step is affine in the state, so a wave's tokens are one
 // factor and one addend; waves meet in LDS, tiles through memory: a tile publishes its factor and
 // addend, then waits for the state before it, which it takes from the nearest of the eight tiles
-// before that has published its own, folded with the factors and addends in between, one after
-// the other, as those tiles do it themselves.  So the same bits come out whoever was first, and a chain of
-// tiles moves on by up to eight a round trip through memory.  The backward does the same from the
-// other end, with the states before the tiles as a forward left them.
+// before (each wave looks at one) that has published its own, folded with the factors and addends in
+// between, one after the other, as those tiles do it themselves.  So the same bits come out whoever was
+// first, and a chain of tiles moves on by up to eight a round trip through memory.  The backward
+// does the same from the other end, with the states before the tiles as a forward left them.
 //
 // Nobody waits for a tile that has not begun: tiles are taken by a counter, in the order of the
 // chain, and a tile's predecessors have smaller numbers.  A published value is a whole word that is
@@ -27,8 +27,8 @@ namespace gdr2 {
 
 namespace {
 
-constexpr int kBack = 8;  // tiles before that are looked at
 constexpr uint32_t kNone = 0xffffffffu;
+constexpr uint32_t kCut = 1, kWait = 2;
 
 // ---- CPL neighbouring channels of a lane, on their way from memory --------------------------
 template <typename T, int CPL>
@@ -65,17 +65,26 @@ __device__ __forceinline__ void rec_put(bf16_t* p, const float (&x)[2]) {
   *reinterpret_cast<bf2*>(p) = bf2{(__bf16)x[0], (__bf16)x[1]};
 }
 
-// a = exp(g), and m = sqrt(1 - a^2) by -expm1(2 g), from its series where 1 - a^2 would cancel:
-// nine terms, (3/4)^9 / 10! < 2^-25 of the first
+// a = exp(g): 2^(k + f) with g log2(e) = k + f, f good to 2^-30; and m = sqrt(1 - a^2) by -expm1(2 g), from its
+// series where 1 - a^2 would cancel: nine terms, (3/4)^9 / 10! < 2^-25 of the first
 template <bool NORM>
 __device__ __forceinline__ void rec_factors(float g, float& a, float& m) {
-  a = expf(g);
+  constexpr float kHigh = 1.44269504f, kLow = 1.92596299e-8f;  // log2(e)
+  const float x = g < -200.f ? -200.f : g;  // (-inf too; exp(-200) is 0 in fp32.  NaN stays.)
+  const float k = rintf(x * kHigh), f = fmaf(x, kLow, fmaf(x, kHigh, -k));
+  a = ldexpf(__builtin_amdgcn_exp2f(f), (int)k);
   m = 1.f;
   if constexpr (NORM) {
     const float y = 2.f * g;
-    float s = 1.f + y * (1.f / 9.f);
-#pragma unroll
-    for (int k = 8; k >= 2; --k) s = fmaf(y * s, 1.f / (float)k, 1.f);
+    float s = 1.f / 362880.f;
+    s = fmaf(s, y, 1.f / 40320.f);
+    s = fmaf(s, y, 1.f / 5040.f);
+    s = fmaf(s, y, 1.f / 720.f);
+    s = fmaf(s, y, 1.f / 120.f);
+    s = fmaf(s, y, 1.f / 24.f);
+    s = fmaf(s, y, 1.f / 6.f);
+    s = fmaf(s, y, 0.5f);
+    s = fmaf(s, y, 1.f);
     m = __builtin_amdgcn_sqrtf(y > -0.75f ? -y * s : fmaf(-a, a, 1.f));
   }
 }
@@ -162,96 +171,130 @@ __device__ __forceinline__ void rec_publish(float* pref, const float (&x)[CPL]) 
     __hip_atomic_store(reinterpret_cast<uint32_t*>(pref) + j, rec_word(x[j]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// One wave's part of the chain, for its lanes' channels c .. c + CPL (on: they exist): tile k takes the
-// state through h -> A h + U.  wait: the state before the tile is asked for, and returned in h;
-// cut: the state behind it does not depend on the one before.
+// What a tile's waves see of the tiles before it, kLook each.
+constexpr int kLook = 2;
+template <int CPL, int NW>
+struct RecLook {
+  float state[kLook * NW][64 * CPL];
+  float2 step[kLook * NW][64 * CPL];
+  int found[kLook * NW];  // 2: the state is there; 1: factor and addend; 0: neither
+};
+
+// Tile k's word to the tiles behind it, from its lanes with channels c .. c + CPL: the state behind it
+// where that does not depend on the one before (final), else factor and addend.
 template <int CPL>
-__device__ __forceinline__ void rec_chain(const RecChain& ch, int D, int k, int c, bool on, bool wait, bool cut,
-                                          const float (&A)[CPL], const float (&U)[CPL], float (&h)[CPL]) {
+__device__ __forceinline__ void rec_announce(const RecChain& ch, int D, int k, int c, bool final, const float (&A)[CPL],
+                                             const float (&U)[CPL]) {
   const size_t at = (size_t)k * D + c;
-  wait = wait && k > 0;  // (offsets that describe no sequences may ask for a state before the first row)
-  if (on) {
-    if (cut || !wait) {
-      rec_publish<CPL>(ch.pref + at, U);
-    } else {
+  if (final) {
+    rec_publish<CPL>(ch.pref + at, U);
+  } else {
 #pragma unroll
-      for (int j = 0; j < CPL; ++j)
-        __hip_atomic_store(reinterpret_cast<uint64_t*>(ch.agg) + at + j, (uint64_t)rec_word(U[j]) << 32 | rec_word(A[j]),
-                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-  }
-#pragma unroll
-  for (int j = 0; j < CPL; ++j) h[j] = 0.f;
-  if (!wait) return;
-  for (bool have = false; !have;) {
-    uint32_t p[kBack][CPL];
-    uint64_t f[kBack][CPL];
-#pragma unroll
-    for (int d = 0; d < kBack; ++d)
-#pragma unroll
-      for (int j = 0; j < CPL; ++j) {
-        const size_t from = (size_t)(k - 1 - d) * D + c + j;
-        p[d][j] = kNone;
-        f[d][j] = ~0ull;
-        if (on && d < k) {
-          p[d][j] = __hip_atomic_load(reinterpret_cast<const uint32_t*>(ch.pref) + from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          if (d < kBack - 1)
-            f[d][j] = __hip_atomic_load(reinterpret_cast<const uint64_t*>(ch.agg) + from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-      }
-#pragma unroll
-    for (int d = kBack - 1; d >= 0; --d) {
-      bool there = true, folds = true;
-#pragma unroll
-      for (int j = 0; j < CPL; ++j) {
-        there = there && p[d][j] != kNone;
-        folds = folds && (uint32_t)f[d][j] != kNone && (uint32_t)(f[d][j] >> 32) != kNone;
-      }
-      if (d < k && __all(there || !on)) {
-        have = true;
-#pragma unroll
-        for (int j = 0; j < CPL; ++j) h[j] = __uint_as_float(p[d][j]);
-      } else if (have && __all(folds || !on)) {
-#pragma unroll
-        for (int j = 0; j < CPL; ++j) h[j] = fmaf(__uint_as_float((uint32_t)f[d][j]), h[j], __uint_as_float((uint32_t)(f[d][j] >> 32)));
-      } else {
-        have = false;
-      }
-    }
-    if (!have) __builtin_amdgcn_s_sleep(2);
-  }
-  if (on && !cut) {
-    float e[CPL];
-#pragma unroll
-    for (int j = 0; j < CPL; ++j) e[j] = fmaf(A[j], h[j], U[j]);
-    rec_publish<CPL>(ch.pref + at, e);
+    for (int j = 0; j < CPL; ++j)
+      __hip_atomic_store(reinterpret_cast<uint64_t*>(ch.agg) + at + j, (uint64_t)rec_word(U[j]) << 32 | rec_word(A[j]),
+                         __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
 }
 
-// the workgroup's number in the chain's order (every lane gets it)
-__device__ __forceinline__ int rec_ticket(uint32_t* counter, bool chained) {
-  if (!chained) return blockIdx.x;
+__device__ __forceinline__ uint32_t rec_peek(const float* pref) {
+  return __hip_atomic_load(reinterpret_cast<const uint32_t*>(pref), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint64_t rec_peek2(const float* agg) {
+  return __hip_atomic_load(reinterpret_cast<const uint64_t*>(agg), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ bool rec_whole(uint64_t f) { return (uint32_t)f != kNone && (uint32_t)(f >> 32) != kNone; }
+
+// The state before tile k > 0, waited for by the whole workgroup (every wave calls it and gets it).
+template <int CPL, int NW>
+__device__ __forceinline__ void rec_await(const RecChain& ch, int D, int k, int c, int col, bool on, int wave,
+                                          RecLook<CPL, NW>& look, float (&h)[CPL]) {
+  const int lane = threadIdx.x & 63;
+  int seen[kLook] = {}, from = -1;
+  for (;;) {
+    uint32_t p[kLook][CPL];
+    uint64_t f[kLook][CPL];
+#pragma unroll
+    for (int q = 0; q < kLook; ++q) {
+      const int d = kLook * wave + q;
+      const size_t at = (size_t)max(k - 1 - d, 0) * D + c;
+      if (on && d < k && seen[q] < 2) {
+#pragma unroll
+        for (int j = 0; j < CPL; ++j) {
+          p[q][j] = rec_peek(ch.pref + at + j);
+          if (seen[q] < 1) f[q][j] = rec_peek2(ch.agg + 2 * (at + j));
+        }
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < kLook; ++q) {
+      const int d = kLook * wave + q;
+      if (d >= k || seen[q] == 2) continue;
+      bool there = true, steps = true;
+      if (on) {
+#pragma unroll
+        for (int j = 0; j < CPL; ++j) {
+          there = there && p[q][j] != kNone;
+          look.state[d][col + j] = __uint_as_float(p[q][j]);
+          if (seen[q] < 1) {
+            steps = steps && rec_whole(f[q][j]);
+            look.step[d][col + j] = float2{__uint_as_float((uint32_t)f[q][j]), __uint_as_float((uint32_t)(f[q][j] >> 32))};
+          }
+        }
+      }
+      seen[q] = __all(there) ? 2 : seen[q] == 1 || __all(steps) ? 1 : 0;
+    }
+    if (lane == 0) {
+#pragma unroll
+      for (int q = 0; q < kLook; ++q) look.found[kLook * wave + q] = seen[q];
+    }
+    __syncthreads();
+    for (int v = 0; v < kLook * NW; ++v) {
+      const int f = __builtin_amdgcn_readfirstlane(look.found[v]);
+      if (f == 2) from = v;
+      if (f != 1) break;
+    }
+    if (from >= 0) break;
+    __builtin_amdgcn_s_sleep(1);
+    __syncthreads();  // everyone has read what is written again
+  }
+#pragma unroll
+  for (int j = 0; j < CPL; ++j) h[j] = look.state[from][col + j];
+  for (int v = from - 1; v >= 0; --v)
+#pragma unroll
+    for (int j = 0; j < CPL; ++j) {
+      const float2 f = look.step[v][col + j];
+      h[j] = fmaf(f.x, h[j], f.y);
+    }
+}
+
+// The workgroup's tile, in the chain's order (every lane gets it), and its group of channels.  A counter
+// for each group, a line apart: one counter for all handed out a tile every 20 ns at best.
+__device__ __forceinline__ int rec_ticket(uint32_t* counters, int groups, int tiles, int& group) {
+  group = (blockIdx.x + blockIdx.x / groups) % groups;
+  if (tiles == 1) return 0;
   __shared__ uint32_t n;
-  if (threadIdx.x == 0) n = atomicAdd(counter, 1u);
+  if (threadIdx.x == 0) n = atomicAdd(counters + 16 * group, 1u);
   __syncthreads();
   return __builtin_amdgcn_readfirstlane((int)n);
 }
 
 }  // namespace
 
-// R tokens a wave, kRecTile / R waves
+// R tokens a wave
 template <typename T, int CPL, int R, bool GATED, bool NORM>
-__global__ __launch_bounds__(64 * kRecTile / R) void rec_fwd_kernel(RecArgs<T> a) {
-  constexpr int NW = kRecTile / R;
-  __shared__ float2 agg[NW][64 * CPL];   // a wave's factor and addend
-  __shared__ float before[NW][64 * CPL]; // the state before a wave's tokens
-  __shared__ uint32_t cuts[NW];          // whether a sequence starts in them
-  const int D = a.D, ncg = (D + 64 * CPL - 1) / (64 * CPL), tiles = (a.rows + kRecTile - 1) / kRecTile;
-  const int n = rec_ticket(a.chain.ticket, tiles > 1), tile = n / ncg;
+__global__ __launch_bounds__(64 * kRecWaves, 4) void rec_fwd_kernel(RecArgs<T> a) {
+  constexpr int NW = kRecWaves, TILE = R * NW;
+  static_assert(kRecBlock % R == 0, "states at waves' ends");
+  __shared__ float2 agg[NW][64 * CPL];  // a wave's factor and addend
+  __shared__ uint32_t cuts[NW];         // whether a sequence starts in its tokens; the first one asks for a state
+  __shared__ RecLook<CPL, NW> look;
+  const int D = a.D, ncg = (D + 64 * CPL - 1) / (64 * CPL), tiles = (a.rows + TILE - 1) / TILE;
+  int group;
+  const int tile = rec_ticket(a.chain.ticket, ncg, tiles, group);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = CPL * lane, c = (n - tile * ncg) * 64 * CPL + col;
+  const int col = CPL * lane, c = group * 64 * CPL + col;
   const bool on = c < D;
-  const int t0 = tile * kRecTile + wave * R, cs = on ? c : 0;
+  const int t0 = tile * TILE + wave * R, cs = on ? c : 0;
 
   RecRaw<T, CPL> rx[R], ri[R];
   RecRaw<float, CPL> rg[R];
@@ -292,15 +335,16 @@ __global__ __launch_bounds__(64 * kRecTile / R) void rec_fwd_kernel(RecArgs<T> a
   }
 #pragma unroll
   for (int j = 0; j < CPL; ++j) agg[wave][col + j] = float2{A[j], U[j]};
-  if (lane == 0) cuts[wave] = w.start;
+  if (lane == 0) cuts[wave] = (w.start != 0 ? kCut : 0) | (rec_bit(w.valid & ~w.start, 0) ? kWait : 0);
   __syncthreads();
-  if (wave == 0) {
-    float At[CPL], Ut[CPL], h[CPL];
-    bool cut = false;
+  const bool wait = tile > 0 && (cuts[0] & kWait) != 0;
+  float At[CPL], Ut[CPL], h[CPL];
+  bool cut = false;
+  if (wave == 0 && tiles > 1) {
 #pragma unroll
     for (int j = 0; j < CPL; ++j) At[j] = 1.f, Ut[j] = 0.f;
     for (int v = 0; v < NW; ++v) {
-      const bool here = __builtin_amdgcn_readfirstlane(cuts[v]) != 0;
+      const bool here = (cuts[v] & kCut) != 0;
       cut = cut || here;
 #pragma unroll
       for (int j = 0; j < CPL; ++j) {
@@ -309,35 +353,39 @@ __global__ __launch_bounds__(64 * kRecTile / R) void rec_fwd_kernel(RecArgs<T> a
         At[j] *= x.x;
       }
     }
+    if (on) rec_announce<CPL>(a.chain, D, tile, c, cut || !wait, At, Ut);
+  }
 #pragma unroll
-    for (int j = 0; j < CPL; ++j) h[j] = 0.f;
-    if (tiles > 1) rec_chain<CPL>(a.chain, D, tile, c, on, rec_bit(w.valid & ~w.start, 0), cut, At, Ut, h);
-    for (int v = 0; v < NW; ++v) {
-      const bool here = __builtin_amdgcn_readfirstlane(cuts[v]) != 0;
+  for (int j = 0; j < CPL; ++j) h[j] = 0.f;
+  if (wait) {
+    rec_await<CPL, NW>(a.chain, D, tile, c, col, on, wave, look, h);
+    if (wave == 0 && on && !cut) {
+      float e[CPL];
 #pragma unroll
-      for (int j = 0; j < CPL; ++j) {
-        const float2 x = agg[v][col + j];
-        before[v][col + j] = h[j];
-        h[j] = here ? x.y : fmaf(x.x, h[j], x.y);
-      }
+      for (int j = 0; j < CPL; ++j) e[j] = fmaf(At[j], h[j], Ut[j]);
+      rec_publish<CPL>(a.chain.pref + (size_t)tile * D + c, e);
     }
   }
-  if (a.o == nullptr) return;
-  __syncthreads();
-  float h[CPL];
+  for (int v = 0; v < wave; ++v) {
+    const bool here = (cuts[v] & kCut) != 0;
 #pragma unroll
-  for (int j = 0; j < CPL; ++j) h[j] = before[wave][col + j];
+    for (int j = 0; j < CPL; ++j) {
+      const float2 x = agg[v][col + j];
+      h[j] = here ? x.y : fmaf(x.x, h[j], x.y);
+    }
+  }
   s = w.first;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
 #pragma unroll
     for (int j = 0; j < CPL; ++j) h[j] = rec_bit(w.start, r) ? u[r][j] : fmaf(al[r][j], h[j], u[r][j]);
-    if (rec_bit(w.valid, r) && on) rec_put(a.o + (size_t)(t0 + r) * D + c, h);
+    if (a.o && rec_bit(w.valid, r) && on) rec_put(a.o + (size_t)(t0 + r) * D + c, h);
     if (rec_bit(w.end, r) && a.hT) {
       s = rec_later(a.cu, a.nseq, a.len, s, t0 + r);
       if (on) rec_put(a.hT + (size_t)s * D + c, h);
     }
   }
+  if (a.states && (t0 + R) % kRecBlock == 0 && t0 < a.rows && on) rec_put(a.states + (size_t)(t0 / kRecBlock) * D + c, h);
   if (a.cu && a.hT)  // empty sequences, shared out over the tiles' waves
     for (int q = tile * NW + wave; q < a.nseq; q += tiles * NW)
       if (a.cu[q + 1] <= a.cu[q] && on) {
@@ -349,18 +397,20 @@ __global__ __launch_bounds__(64 * kRecTile / R) void rec_fwd_kernel(RecArgs<T> a
 }
 
 template <typename T, int CPL, int R, bool GATED, bool NORM>
-__global__ __launch_bounds__(64 * kRecTile / R) void rec_bwd_kernel(RecBwdArgs<T> a) {
-  constexpr int NW = kRecTile / R;
+__global__ __launch_bounds__(64 * kRecWaves, 4) void rec_bwd_kernel(RecBwdArgs<T> a) {
+  constexpr int NW = kRecWaves, TILE = R * NW;
+  static_assert(TILE == kRecBlock, "a tile starts at a stored state");
   __shared__ float2 agg[NW][64 * CPL];   // forward
   __shared__ float radd[NW][64 * CPL];   // backward: the addend (the factor is the same)
-  __shared__ float before[NW][64 * CPL], behind[NW][64 * CPL];
   __shared__ uint32_t cuts[NW], rcuts[NW];
-  const int D = a.D, ncg = (D + 64 * CPL - 1) / (64 * CPL), tiles = (a.rows + kRecTile - 1) / kRecTile;
-  const int n = rec_ticket(a.chain.ticket, tiles > 1), k = n / ncg, tile = tiles - 1 - k;
+  __shared__ RecLook<CPL, NW> look;
+  const int D = a.D, ncg = (D + 64 * CPL - 1) / (64 * CPL), tiles = (a.rows + TILE - 1) / TILE;
+  int group;
+  const int k = rec_ticket(a.chain.ticket, ncg, tiles, group), tile = tiles - 1 - k;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = CPL * lane, c = (n - k * ncg) * 64 * CPL + col;
+  const int col = CPL * lane, c = group * 64 * CPL + col;
   const bool on = c < D;
-  const int t0 = tile * kRecTile + wave * R, cs = on ? c : 0;
+  const int t0 = tile * TILE + wave * R, cs = on ? c : 0;
 
   RecRaw<T, CPL> rx[R], ri[R], rd[R];
   RecRaw<float, CPL> rg[R];
@@ -414,29 +464,23 @@ __global__ __launch_bounds__(64 * kRecTile / R) void rec_bwd_kernel(RecBwdArgs<T
   }
 #pragma unroll
   for (int j = 0; j < CPL; ++j) radd[wave][col + j] = U[j];
-  if (lane == 0) cuts[wave] = w.start, rcuts[wave] = w.end;
-  __syncthreads();
-  if (wave == 1 % NW) {  // the states before the waves' rows
-    float h[CPL];
-#pragma unroll
-    for (int j = 0; j < CPL; ++j) h[j] = tile > 0 && on ? a.states[(size_t)(tile - 1) * D + c + j] : 0.f;
-    for (int v = 0; v < NW; ++v) {
-      const bool here = __builtin_amdgcn_readfirstlane(cuts[v]) != 0;
-#pragma unroll
-      for (int j = 0; j < CPL; ++j) {
-        const float2 x = agg[v][col + j];
-        before[v][col + j] = h[j];
-        h[j] = here ? x.y : fmaf(x.x, h[j], x.y);
-      }
-    }
+  if (lane == 0) {
+    cuts[wave] = w.start != 0 ? kCut : 0;
+    rcuts[wave] = (w.end != 0 ? kCut : 0) | (rec_bit(w.valid & ~w.end, R - 1) ? kWait : 0);
   }
-  if (wave == NW - 1) {  // the gradients behind them; this wave's last row is the tile's
-    float At[CPL], Ut[CPL], h[CPL];
-    bool cut = false;
+  float h[CPL];  // the state before the tile
+#pragma unroll
+  for (int j = 0; j < CPL; ++j) h[j] = tile > 0 && on ? a.states[(size_t)(tile - 1) * D + c + j] : 0.f;
+  __syncthreads();
+  // the gradient behind the tile's last row, from the other end
+  const bool wait = k > 0 && (rcuts[NW - 1] & kWait) != 0;
+  float At[CPL], Ut[CPL], back[CPL];
+  bool cut = false;
+  if (wave == 0 && tiles > 1) {
 #pragma unroll
     for (int j = 0; j < CPL; ++j) At[j] = 1.f, Ut[j] = 0.f;
     for (int v = NW - 1; v >= 0; --v) {
-      const bool here = __builtin_amdgcn_readfirstlane(rcuts[v]) != 0;
+      const bool here = (rcuts[v] & kCut) != 0;
       cut = cut || here;
 #pragma unroll
       for (int j = 0; j < CPL; ++j) {
@@ -445,23 +489,36 @@ __global__ __launch_bounds__(64 * kRecTile / R) void rec_bwd_kernel(RecBwdArgs<T
         At[j] *= f;
       }
     }
+    if (on) rec_announce<CPL>(a.chain, D, k, c, cut || !wait, At, Ut);
+  }
 #pragma unroll
-    for (int j = 0; j < CPL; ++j) h[j] = 0.f;
-    if (tiles > 1) rec_chain<CPL>(a.chain, D, k, c, on, rec_bit(w.valid & ~w.end, R - 1), cut, At, Ut, h);
-    for (int v = NW - 1; v >= 0; --v) {
-      const bool here = __builtin_amdgcn_readfirstlane(rcuts[v]) != 0;
+  for (int j = 0; j < CPL; ++j) back[j] = 0.f;
+  if (wait) {
+    rec_await<CPL, NW>(a.chain, D, k, c, col, on, wave, look, back);
+    if (wave == 0 && on && !cut) {
+      float e[CPL];
 #pragma unroll
-      for (int j = 0; j < CPL; ++j) {
-        const float f = agg[v][col + j].x, b = radd[v][col + j];
-        behind[v][col + j] = h[j];
-        h[j] = here ? b : fmaf(f, h[j], b);
-      }
+      for (int j = 0; j < CPL; ++j) e[j] = fmaf(At[j], back[j], Ut[j]);
+      rec_publish<CPL>(a.chain.pref + (size_t)k * D + c, e);
     }
   }
-  __syncthreads();
-  float h[CPL], hb[R][CPL];
+  for (int v = NW - 1; v > wave; --v) {
+    const bool here = (rcuts[v] & kCut) != 0;
 #pragma unroll
-  for (int j = 0; j < CPL; ++j) h[j] = before[wave][col + j];
+    for (int j = 0; j < CPL; ++j) {
+      const float b = radd[v][col + j];
+      back[j] = here ? b : fmaf(agg[v][col + j].x, back[j], b);
+    }
+  }
+  float hb[R][CPL];
+  for (int v = 0; v < wave; ++v) {
+    const bool here = (cuts[v] & kCut) != 0;
+#pragma unroll
+    for (int j = 0; j < CPL; ++j) {
+      const float2 x = agg[v][col + j];
+      h[j] = here ? x.y : fmaf(x.x, h[j], x.y);
+    }
+  }
   s = w.first;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
@@ -476,7 +533,7 @@ __global__ __launch_bounds__(64 * kRecTile / R) void rec_bwd_kernel(RecBwdArgs<T
     }
   }
 #pragma unroll
-  for (int j = 0; j < CPL; ++j) h[j] = behind[wave][col + j];
+  for (int j = 0; j < CPL; ++j) h[j] = back[j];
   s = w.last;
 #pragma unroll
   for (int r = R - 1; r >= 0; --r) {
@@ -495,7 +552,7 @@ __global__ __launch_bounds__(64 * kRecTile / R) void rec_bwd_kernel(RecBwdArgs<T
       di[j] = md * x;
       dg[j] = h[j] * hb[r][j];
       if constexpr (NORM) {
-        const float slope = m[r][j] > 0.f ? al[r][j] * al[r][j] / m[r][j] : 0.f;
+        const float slope = m[r][j] > 0.f ? al[r][j] * al[r][j] * __builtin_amdgcn_rcpf(m[r][j]) : 0.f;
         dg[j] -= slope * i * x * dh;
       }
     }
@@ -552,18 +609,17 @@ __global__ __launch_bounds__(256) void rec_step_kernel(RecStepArgs<T> a) {
   a.h[(size_t)s * a.D + c] = h;
 }
 
-__global__ __launch_bounds__(256) void rec_clear_kernel(u4v* p, size_t words) {
-  u4v* chain = p + blockIdx.y * words;
+__global__ __launch_bounds__(256) void rec_clear_kernel(u4v* p, size_t words, size_t zeros) {
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < words; i += (size_t)gridDim.x * 256) {
-    const uint32_t v = i < 16 ? 0u : kNone;
-    chain[i] = u4v{v, v, v, v};
+    const uint32_t v = i < zeros ? 0u : kNone;
+    p[i] = u4v{v, v, v, v};
   }
 }
 
-hipError_t launch_rec_clear(void* p, size_t words, int chains, hipStream_t st) {
+hipError_t launch_rec_clear(void* p, size_t words, size_t zeros, hipStream_t st) {
   const size_t blocks = (words + 255) / 256;
-  hipLaunchKernelGGL(rec_clear_kernel, dim3((unsigned)(blocks < 2048 ? blocks : 2048), chains), dim3(256), 0, st,
-                     static_cast<u4v*>(p), words);
+  hipLaunchKernelGGL(rec_clear_kernel, dim3((unsigned)(blocks < 2048 ? blocks : 2048)), dim3(256), 0, st,
+                     static_cast<u4v*>(p), words, zeros);
   return hipGetLastError();
 }
 
@@ -574,35 +630,42 @@ hipError_t rec_options(bool gated, bool norm, F&& f) {
   if (gated) return norm ? f(std::true_type{}, std::true_type{}) : f(std::true_type{}, std::false_type{});
   return norm ? f(std::false_type{}, std::true_type{}) : f(std::false_type{}, std::false_type{});
 }
-template <int CPL>
-unsigned rec_blocks(int rows, int D) {
-  return (unsigned)((rows + kRecTile - 1) / kRecTile) * (unsigned)((D + 64 * CPL - 1) / (64 * CPL));
+unsigned rec_blocks(int rows, int tile, int D) {
+  return (unsigned)((rows + tile - 1) / tile) * (unsigned)((D + rec_channels(D) - 1) / rec_channels(D));
 }
 }  // namespace
 
 template <typename T>
 hipError_t launch_rec_fwd(const RecArgs<T>& a, hipStream_t st) {
-  constexpr int R = 16;
+  const int tile = rec_tile(a.rows, a.D);
+  const dim3 grid(rec_blocks(a.rows, tile, a.D)), block(64 * kRecWaves);
   return rec_options(a.i != nullptr, a.normalize != 0, [&](auto gated, auto norm) {
-    if (a.D % 2 == 0 && a.D > 64)
-      hipLaunchKernelGGL((rec_fwd_kernel<T, 2, R, decltype(gated)::value, decltype(norm)::value>), dim3(rec_blocks<2>(a.rows, a.D)),
-                         dim3(64 * kRecTile / R), 0, st, a);
-    else
-      hipLaunchKernelGGL((rec_fwd_kernel<T, 1, R, decltype(gated)::value, decltype(norm)::value>), dim3(rec_blocks<1>(a.rows, a.D)),
-                         dim3(64 * kRecTile / R), 0, st, a);
+    constexpr bool G = decltype(gated)::value, N = decltype(norm)::value;
+    constexpr int R = kRecTile / kRecWaves;
+    if (rec_channels(a.D) == 128) {
+      if (tile == kRecTile)
+        hipLaunchKernelGGL((rec_fwd_kernel<T, 2, R, G, N>), grid, block, 0, st, a);
+      else
+        hipLaunchKernelGGL((rec_fwd_kernel<T, 2, R / 2, G, N>), grid, block, 0, st, a);
+    } else {
+      if (tile == kRecTile)
+        hipLaunchKernelGGL((rec_fwd_kernel<T, 1, R, G, N>), grid, block, 0, st, a);
+      else
+        hipLaunchKernelGGL((rec_fwd_kernel<T, 1, R / 2, G, N>), grid, block, 0, st, a);
+    }
     return hipGetLastError();
   });
 }
 template <typename T>
 hipError_t launch_rec_bwd(const RecBwdArgs<T>& a, hipStream_t st) {
-  constexpr int R = 8;
+  const dim3 grid(rec_blocks(a.rows, kRecBlock, a.D)), block(64 * kRecWaves);
   return rec_options(a.i != nullptr, a.normalize != 0, [&](auto gated, auto norm) {
-    if (a.D % 2 == 0 && a.D > 64)
-      hipLaunchKernelGGL((rec_bwd_kernel<T, 2, R, decltype(gated)::value, decltype(norm)::value>), dim3(rec_blocks<2>(a.rows, a.D)),
-                         dim3(64 * kRecTile / R), 0, st, a);
+    constexpr bool G = decltype(gated)::value, N = decltype(norm)::value;
+    constexpr int R = kRecBlock / kRecWaves;
+    if (rec_channels(a.D) == 128)
+      hipLaunchKernelGGL((rec_bwd_kernel<T, 2, R, G, N>), grid, block, 0, st, a);
     else
-      hipLaunchKernelGGL((rec_bwd_kernel<T, 1, R, decltype(gated)::value, decltype(norm)::value>), dim3(rec_blocks<1>(a.rows, a.D)),
-                         dim3(64 * kRecTile / R), 0, st, a);
+      hipLaunchKernelGGL((rec_bwd_kernel<T, 1, R, G, N>), grid, block, 0, st, a);
     return hipGetLastError();
   });
 }

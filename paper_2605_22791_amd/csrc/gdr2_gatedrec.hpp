@@ -6,7 +6,18 @@
 
 namespace gdr2 {
 
-constexpr int kRecTile = 128;  // tokens of a workgroup's tile, forward and backward
+constexpr int kRecWaves = 8;    // waves of a workgroup
+constexpr int kRecBlock = 64;   // tokens of a workgroup of the backward, which starts from the states between them
+constexpr int kRecTile = 128;   // and of the forward, half of it where that leaves few workgroups
+
+// Channels of a workgroup: two a lane where their pairs are aligned and fill a wave.
+inline int rec_channels(int D) { return D % 2 == 0 && D > 64 ? 128 : 64; }
+// Tokens of a forward workgroup.  Tiles of 128 make a shorter chain (65536 tokens of 2048 channels: 257 us,
+// 334 with 64); eight workgroups a CU are needed to hide their waits (9 packed prompts of 8192 tokens, four
+// a CU with 128: 62 us, 57 with 64).
+inline int rec_tile(int64_t rows, int D) {
+  return (rows + kRecTile - 1) / kRecTile * ((D + rec_channels(D) - 1) / rec_channels(D)) >= 2048 ? kRecTile : kRecTile / 2;
+}
 
 // What tiles hand to the tiles behind them, in the order in which they are taken: pref (tiles, D) the
 // state behind a tile, agg (tiles, D, 2) the factor and the addend that a tile takes it there by.
@@ -14,7 +25,7 @@ constexpr int kRecTile = 128;  // tokens of a workgroup's tile, forward and back
 struct RecChain {
   float* pref;
   float* agg;
-  uint32_t* ticket;  // the next tile to take; zero before the launch
+  uint32_t* ticket;  // the next tile to take, a word in 16 for every group of channels; zero before the launch
 };
 
 template <typename T>
@@ -22,8 +33,9 @@ struct RecArgs {
   const T *x, *i;       // i nullable
   const float *g, *h0;  // h0 nullable
   const int32_t* cu;    // packed: nseq + 1 offsets; else NULL
-  T* o;                 // nullable: the chain's states alone
+  T* o;                 // nullable: the states alone
   float* hT;            // nullable
+  float* states;        // nullable: behind every kRecBlock tokens, (blocks, D)
   RecChain chain;
   int nseq, len;        // sequences; tokens of one (fixed length) or of the batch
   int rows, D, normalize;
@@ -33,7 +45,7 @@ template <typename T>
 struct RecBwdArgs {
   const T *x, *i, *dout;
   const float *g, *h0, *dhT;
-  const float* states;  // behind every tile, (tiles, D)
+  const float* states;  // behind every kRecBlock tokens, (blocks, D)
   const int32_t* cu;
   T *dx, *di;
   float *dg, *dh0;
@@ -59,7 +71,7 @@ template <typename T>
 hipError_t launch_rec_bwd(const RecBwdArgs<T>& a, hipStream_t st);
 template <typename T>
 hipError_t launch_rec_step(const RecStepArgs<T>& a, hipStream_t st);
-// `chains` chains of `words` 16-byte words each: all ones, the first 256 bytes zero
-hipError_t launch_rec_clear(void* p, size_t words, int chains, hipStream_t st);
+// `words` 16-byte words of all ones, but zero the first `zeros`
+hipError_t launch_rec_clear(void* p, size_t words, size_t zeros, hipStream_t st);
 
 }  // namespace gdr2

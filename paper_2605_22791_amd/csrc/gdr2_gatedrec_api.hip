@@ -21,34 +21,48 @@ gdr2_status rec_check(const gdr2_gatedrec* p, const int32_t* cu, int nseq, bool 
   if (p->D > kMaxChannels || nseq > kMaxSeqs) return GDR2_EUNSUPPORTED;
   if ((double)p->B * p->T >= 2147483648.0) return GDR2_EUNSUPPORTED;
   // workgroups of one launch: (tile, 64 channels) and, token by token, (sequence, 256 channels)
-  if (((double)p->B * p->T / kRecTile + 1) * ((p->D + 63) / 64) >= 2147483648.0) return GDR2_EUNSUPPORTED;
+  if (((double)p->B * p->T / kRecBlock + 1) * ((p->D + 63) / 64) >= 2147483648.0) return GDR2_EUNSUPPORTED;
   if ((double)(nseq > 0 ? nseq : p->B) * ((p->D + 255) / 256) >= 2147483648.0) return GDR2_EUNSUPPORTED;
   return GDR2_OK;
 }
 
-// Workspace: the forward chain (a line for its counter, states behind the tiles, factors and
-// addends), and for a backward the reverse chain behind it.  One tile needs no chain.
+// Workspace: the chains of the forward's and the backward's tiles (counters, states behind the tiles,
+// factors and addends), and the states that a backward starts from.  One tile needs no chain.
 struct RecLayout {
-  size_t half, pref, agg, total;  // one chain's bytes, and the offsets in it
-  int tiles;
+  struct Chain {
+    size_t at, pref, agg, bytes;
+    int tiles;
+  } chain[2];  // forward, backward
+  size_t states, total;
 };
 RecLayout rec_layout(const gdr2_gatedrec* p, bool bwd) {
   RecLayout L{};
-  L.tiles = (int)(((int64_t)p->B * p->T + kRecTile - 1) / kRecTile);
-  const size_t n = (size_t)L.tiles * p->D;
-  L.pref = kAlign;
-  L.agg = L.pref + round_up(4 * n);
-  L.half = L.tiles > 1 ? L.agg + round_up(8 * n) : kAlign;
-  L.total = (bwd ? 2 : 1) * L.half;
+  const int64_t rows = (int64_t)p->B * p->T;
+  size_t off = 0;
+  for (int k = 0; k < (bwd ? 2 : 1); ++k) {
+    RecLayout::Chain& c = L.chain[k];
+    const int tile = k == 0 ? rec_tile(rows, p->D) : kRecBlock;
+    c.tiles = (int)((rows + tile - 1) / tile);
+    c.at = off;
+    if (c.tiles > 1) {
+      const size_t n = (size_t)c.tiles * p->D;
+      c.pref = round_up((size_t)(p->D + 63) / 64 * 64);  // a counter for 64 channels, 64 bytes apart
+      c.agg = c.pref + round_up(4 * n);
+      c.bytes = c.agg + round_up(8 * n);
+    }
+    off += c.bytes;
+  }
+  L.states = off;
+  if (bwd) off += round_up((size_t)L.chain[1].tiles * p->D * 4);
+  L.total = off + kAlign;
   return L;
 }
-RecChain rec_chain_at(void* ws, size_t off, const RecLayout& L) {
-  return {at<float>(ws, off + L.pref), at<float>(ws, off + L.agg), at<uint32_t>(ws, off)};
+RecChain rec_chain_at(void* ws, const RecLayout::Chain& c) {
+  return {at<float>(ws, c.at + c.pref), at<float>(ws, c.at + c.agg), at<uint32_t>(ws, c.at)};
 }
-// chains [from, to) of the workspace as a launch finds them: nothing published, counters at zero
-hipError_t rec_clear(void* ws, const RecLayout& L, int from, int to, hipStream_t st) {
-  if (L.tiles <= 1) return hipSuccess;
-  return launch_rec_clear(at<char>(ws, from * L.half), L.half / 16, to - from, st);
+// a chain as a launch finds it: nothing published, counters at zero
+hipError_t rec_clear(void* ws, const RecLayout::Chain& c, hipStream_t st) {
+  return c.tiles > 1 ? launch_rec_clear(at<char>(ws, c.at), c.bytes / 16, c.pref / 16, st) : hipSuccess;
 }
 
 bool need(const void* x) { return x != nullptr && aligned16(x); }
@@ -65,7 +79,9 @@ void rec_shape(A& a, const gdr2_gatedrec* p, const int32_t* cu, int n) {
 
 template <typename T>
 hipError_t rec_fwd(const gdr2_gatedrec* p, const int32_t* cu, int n, const void* x, const float* g, const void* i,
-                   const float* h0, void* o, float* hT, const RecChain& chain, hipStream_t st) {
+                   const float* h0, void* o, float* hT, const RecLayout& L, void* ws, bool save, hipStream_t st) {
+  const hipError_t e = rec_clear(ws, L.chain[0], st);
+  if (e != hipSuccess) return e;
   RecArgs<T> a{};
   rec_shape(a, p, cu, n);
   a.x = static_cast<const T*>(x);
@@ -74,7 +90,8 @@ hipError_t rec_fwd(const gdr2_gatedrec* p, const int32_t* cu, int n, const void*
   a.h0 = h0;
   a.o = static_cast<T*>(o);
   a.hT = hT;
-  a.chain = chain;
+  a.states = save ? at<float>(ws, L.states) : nullptr;
+  a.chain = rec_chain_at(ws, L.chain[0]);
   a.rows = p->B * p->T;
   return launch_rec_fwd<T>(a, st);
 }
@@ -112,11 +129,8 @@ gdr2_status gdr2_gatedrec_fwd(const gdr2_gatedrec* p, const int32_t* cu, int32_t
   if (!need(x) || !need(g) || !aligned16(i) || !aligned16(h0) || !need(o) || !aligned16(hT) || !need(ws)) return GDR2_EINVAL;
   const RecLayout L = rec_layout(p, save != 0);
   if (ws_bytes < L.total) return GDR2_EWORKSPACE;
-  const RecChain chain = rec_chain_at(ws, 0, L);
-  hipError_t e = rec_clear(ws, L, 0, 1, stream);
-  if (e == hipSuccess)
-    e = p->dtype == GDR2_FP32 ? rec_fwd<float>(p, cu, n, x, g, i, h0, o, hT, chain, stream)
-                              : rec_fwd<bf16_t>(p, cu, n, x, g, i, h0, o, hT, chain, stream);
+  const hipError_t e = p->dtype == GDR2_FP32 ? rec_fwd<float>(p, cu, n, x, g, i, h0, o, hT, L, ws, save != 0, stream)
+                                             : rec_fwd<bf16_t>(p, cu, n, x, g, i, h0, o, hT, L, ws, save != 0, stream);
   return hip_status(e, stream);
 }
 
@@ -133,9 +147,9 @@ gdr2_status gdr2_gatedrec_bwd(const gdr2_gatedrec* p, const int32_t* cu, int32_t
   if (ws_bytes < L.total) return GDR2_EWORKSPACE;
   const auto run = [&](auto t) {
     using T = decltype(t);
-    const RecChain forward = rec_chain_at(ws, 0, L);
-    hipError_t e = rec_clear(ws, L, saved ? 1 : 0, 2, stream);
-    if (e == hipSuccess && !saved && L.tiles > 1) e = rec_fwd<T>(p, cu, n, x, g, i, h0, nullptr, nullptr, forward, stream);
+    hipError_t e = hipSuccess;
+    if (!saved && L.chain[1].tiles > 1) e = rec_fwd<T>(p, cu, n, x, g, i, h0, nullptr, nullptr, L, ws, true, stream);
+    if (e == hipSuccess) e = rec_clear(ws, L.chain[1], stream);
     if (e != hipSuccess) return e;
     RecBwdArgs<T> a{};
     rec_shape(a, p, cu, n);
@@ -145,12 +159,12 @@ gdr2_status gdr2_gatedrec_bwd(const gdr2_gatedrec* p, const int32_t* cu, int32_t
     a.g = g;
     a.h0 = h0;
     a.dhT = dhT;
-    a.states = forward.pref;
+    a.states = at<float>(ws, L.states);
     a.dx = static_cast<T*>(dx);
     a.di = static_cast<T*>(di);
     a.dg = dg;
     a.dh0 = dh0;
-    a.chain = rec_chain_at(ws, L.half, L);
+    a.chain = rec_chain_at(ws, L.chain[1]);
     a.rows = p->B * p->T;
     return launch_rec_bwd<T>(a, stream);
   };
