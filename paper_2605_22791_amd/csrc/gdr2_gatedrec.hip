@@ -171,13 +171,12 @@ __device__ __forceinline__ void rec_publish(float* pref, const float (&x)[CPL]) 
     __hip_atomic_store(reinterpret_cast<uint32_t*>(pref) + j, rec_word(x[j]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// What a tile's waves see of the tiles before it, kLook each.
-constexpr int kLook = 2;
+// What a tile's waves see of the tiles before it, one each (two or four each took 3 to 10 % longer).
 template <int CPL, int NW>
 struct RecLook {
-  float state[kLook * NW][64 * CPL];
-  float2 step[kLook * NW][64 * CPL];
-  int found[kLook * NW];  // 2: the state is there; 1: factor and addend; 0: neither
+  float state[NW][64 * CPL];
+  float2 step[NW][64 * CPL];
+  int found[NW];  // 2: the state is there; 1: factor and addend; 0: neither
 };
 
 // Tile k's word to the tiles behind it, from its lanes with channels c .. c + CPL: the state behind it
@@ -209,46 +208,35 @@ template <int CPL, int NW>
 __device__ __forceinline__ void rec_await(const RecChain& ch, int D, int k, int c, int col, bool on, int wave,
                                           RecLook<CPL, NW>& look, float (&h)[CPL]) {
   const int lane = threadIdx.x & 63;
-  int seen[kLook] = {}, from = -1;
+  const int d = wave;
+  const size_t at = (size_t)max(k - 1 - d, 0) * D + c;
+  int seen = 0, from = -1;
   for (;;) {
-    uint32_t p[kLook][CPL];
-    uint64_t f[kLook][CPL];
-#pragma unroll
-    for (int q = 0; q < kLook; ++q) {
-      const int d = kLook * wave + q;
-      const size_t at = (size_t)max(k - 1 - d, 0) * D + c;
-      if (on && d < k && seen[q] < 2) {
-#pragma unroll
-        for (int j = 0; j < CPL; ++j) {
-          p[q][j] = rec_peek(ch.pref + at + j);
-          if (seen[q] < 1) f[q][j] = rec_peek2(ch.agg + 2 * (at + j));
-        }
-      }
-    }
-#pragma unroll
-    for (int q = 0; q < kLook; ++q) {
-      const int d = kLook * wave + q;
-      if (d >= k || seen[q] == 2) continue;
+    if (d < k && seen < 2) {
       bool there = true, steps = true;
       if (on) {
+        uint32_t p[CPL];
+        uint64_t f[CPL];
 #pragma unroll
         for (int j = 0; j < CPL; ++j) {
-          there = there && p[q][j] != kNone;
-          look.state[d][col + j] = __uint_as_float(p[q][j]);
-          if (seen[q] < 1) {
-            steps = steps && rec_whole(f[q][j]);
-            look.step[d][col + j] = float2{__uint_as_float((uint32_t)f[q][j]), __uint_as_float((uint32_t)(f[q][j] >> 32))};
+          p[j] = rec_peek(ch.pref + at + j);
+          if (seen < 1) f[j] = rec_peek2(ch.agg + 2 * (at + j));
+        }
+#pragma unroll
+        for (int j = 0; j < CPL; ++j) {
+          there = there && p[j] != kNone;
+          look.state[d][col + j] = __uint_as_float(p[j]);
+          if (seen < 1) {
+            steps = steps && rec_whole(f[j]);
+            look.step[d][col + j] = float2{__uint_as_float((uint32_t)f[j]), __uint_as_float((uint32_t)(f[j] >> 32))};
           }
         }
       }
-      seen[q] = __all(there) ? 2 : seen[q] == 1 || __all(steps) ? 1 : 0;
+      seen = __all(there) ? 2 : seen == 1 || __all(steps) ? 1 : 0;
     }
-    if (lane == 0) {
-#pragma unroll
-      for (int q = 0; q < kLook; ++q) look.found[kLook * wave + q] = seen[q];
-    }
+    if (lane == 0) look.found[d] = seen;
     __syncthreads();
-    for (int v = 0; v < kLook * NW; ++v) {
+    for (int v = 0; v < NW; ++v) {
       const int f = __builtin_amdgcn_readfirstlane(look.found[v]);
       if (f == 2) from = v;
       if (f != 1) break;
@@ -609,17 +597,19 @@ __global__ __launch_bounds__(256) void rec_step_kernel(RecStepArgs<T> a) {
   a.h[(size_t)s * a.D + c] = h;
 }
 
-__global__ __launch_bounds__(256) void rec_clear_kernel(u4v* p, size_t words, size_t zeros) {
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < words; i += (size_t)gridDim.x * 256) {
-    const uint32_t v = i < zeros ? 0u : kNone;
+__global__ __launch_bounds__(256) void rec_clear_kernel(RecClear x, RecClear y) {
+  const RecClear& c = blockIdx.y == 0 ? x : y;
+  u4v* p = static_cast<u4v*>(c.p);
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < c.words; i += (size_t)gridDim.x * 256) {
+    const uint32_t v = i < c.zeros ? 0u : kNone;
     p[i] = u4v{v, v, v, v};
   }
 }
 
-hipError_t launch_rec_clear(void* p, size_t words, size_t zeros, hipStream_t st) {
-  const size_t blocks = (words + 255) / 256;
-  hipLaunchKernelGGL(rec_clear_kernel, dim3((unsigned)(blocks < 2048 ? blocks : 2048)), dim3(256), 0, st,
-                     static_cast<u4v*>(p), words, zeros);
+hipError_t launch_rec_clear(const RecClear& x, const RecClear& y, hipStream_t st) {
+  const size_t words = x.words > y.words ? x.words : y.words, blocks = (words + 255) / 256;
+  if (words == 0) return hipSuccess;
+  hipLaunchKernelGGL(rec_clear_kernel, dim3((unsigned)(blocks < 2048 ? blocks : 2048), y.words > 0 ? 2 : 1), dim3(256), 0, st, x, y);
   return hipGetLastError();
 }
 

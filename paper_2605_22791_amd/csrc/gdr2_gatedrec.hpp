@@ -71,7 +71,11 @@ template <typename T>
 hipError_t launch_rec_bwd(const RecBwdArgs<T>& a, hipStream_t st);
 template <typename T>
 hipError_t launch_rec_step(const RecStepArgs<T>& a, hipStream_t st);
-// `words` 16-byte words of all ones, but zero the first `zeros`
-hipError_t launch_rec_clear(void* p, size_t words, size_t zeros, hipStream_t st);
+// `words` 16-byte words of all ones, but zero the first `zeros`: a chain as a launch finds it
+struct RecClear {
+  void* p;
+  size_t words, zeros;
+};
+hipError_t launch_rec_clear(const RecClear& x, const RecClear& y, hipStream_t st);
 
 }  // namespace gdr2

@@ -60,10 +60,7 @@ RecLayout rec_layout(const gdr2_gatedrec* p, bool bwd) {
 RecChain rec_chain_at(void* ws, const RecLayout::Chain& c) {
   return {at<float>(ws, c.at + c.pref), at<float>(ws, c.at + c.agg), at<uint32_t>(ws, c.at)};
 }
-// a chain as a launch finds it: nothing published, counters at zero
-hipError_t rec_clear(void* ws, const RecLayout::Chain& c, hipStream_t st) {
-  return c.tiles > 1 ? launch_rec_clear(at<char>(ws, c.at), c.bytes / 16, c.pref / 16, st) : hipSuccess;
-}
+RecClear rec_clear(void* ws, const RecLayout::Chain& c) { return {at<char>(ws, c.at), c.bytes / 16, c.pref / 16}; }
 
 bool need(const void* x) { return x != nullptr && aligned16(x); }
 
@@ -80,8 +77,6 @@ void rec_shape(A& a, const gdr2_gatedrec* p, const int32_t* cu, int n) {
 template <typename T>
 hipError_t rec_fwd(const gdr2_gatedrec* p, const int32_t* cu, int n, const void* x, const float* g, const void* i,
                    const float* h0, void* o, float* hT, const RecLayout& L, void* ws, bool save, hipStream_t st) {
-  const hipError_t e = rec_clear(ws, L.chain[0], st);
-  if (e != hipSuccess) return e;
   RecArgs<T> a{};
   rec_shape(a, p, cu, n);
   a.x = static_cast<const T*>(x);
@@ -129,8 +124,10 @@ gdr2_status gdr2_gatedrec_fwd(const gdr2_gatedrec* p, const int32_t* cu, int32_t
   if (!need(x) || !need(g) || !aligned16(i) || !aligned16(h0) || !need(o) || !aligned16(hT) || !need(ws)) return GDR2_EINVAL;
   const RecLayout L = rec_layout(p, save != 0);
   if (ws_bytes < L.total) return GDR2_EWORKSPACE;
-  const hipError_t e = p->dtype == GDR2_FP32 ? rec_fwd<float>(p, cu, n, x, g, i, h0, o, hT, L, ws, save != 0, stream)
-                                             : rec_fwd<bf16_t>(p, cu, n, x, g, i, h0, o, hT, L, ws, save != 0, stream);
+  hipError_t e = launch_rec_clear(rec_clear(ws, L.chain[0]), {}, stream);
+  if (e == hipSuccess)
+    e = p->dtype == GDR2_FP32 ? rec_fwd<float>(p, cu, n, x, g, i, h0, o, hT, L, ws, save != 0, stream)
+                              : rec_fwd<bf16_t>(p, cu, n, x, g, i, h0, o, hT, L, ws, save != 0, stream);
   return hip_status(e, stream);
 }
 
@@ -147,9 +144,9 @@ gdr2_status gdr2_gatedrec_bwd(const gdr2_gatedrec* p, const int32_t* cu, int32_t
   if (ws_bytes < L.total) return GDR2_EWORKSPACE;
   const auto run = [&](auto t) {
     using T = decltype(t);
-    hipError_t e = hipSuccess;
-    if (!saved && L.chain[1].tiles > 1) e = rec_fwd<T>(p, cu, n, x, g, i, h0, nullptr, nullptr, L, ws, true, stream);
-    if (e == hipSuccess) e = rec_clear(ws, L.chain[1], stream);
+    const bool states = !saved && L.chain[1].tiles > 1;
+    hipError_t e = launch_rec_clear(rec_clear(ws, L.chain[1]), states ? rec_clear(ws, L.chain[0]) : RecClear{}, stream);
+    if (e == hipSuccess && states) e = rec_fwd<T>(p, cu, n, x, g, i, h0, nullptr, nullptr, L, ws, true, stream);
     if (e != hipSuccess) return e;
     RecBwdArgs<T> a{};
     rec_shape(a, p, cu, n);
