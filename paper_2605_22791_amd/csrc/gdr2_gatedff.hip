@@ -1,5 +1,21 @@
-// Gated feed-forward block: the products, fp32 accumulation on the matrix cores, and the
-// activation with its gradient.
+// Gated feed-forward block (include/gdr2_gatedff.h): one product kernel for its six products.
+//
+// A workgroup takes a tile of C, 256 x 256 in eight waves or 128 x 128 in four, through K in steps of
+// 128 bytes (64 bf16, 32 fp32): the next step's tiles of A and B come straight into LDS while the
+// matrix cores work on this one's.  bf16 products are v_mfma_f32_16x16x32_bf16, fp32 ones
+// v_mfma_f32_16x16x4_f32; the operands change places, so that a lane has four neighbouring columns of
+// C.  Operands with their sum along the rows are read as 16-byte fragments, the others (bf16) through
+// the transposing load; both are stored with their 16-byte pieces exchanged within a row so that
+// neither way of reading meets a bank twice.
+//
+// Tiles that are left over when every CU has had the same number are cut along K so that all CUs have a
+// part of them; parts meet in a second launch, in order.  Values past a matrix's end come as zeros
+// from the buffer loads' range check, and pieces past the end of the sum are sent out of range.
+//
+// C leaves through LDS, 16 rows of a wave at a time, so that memory sees whole rows of a tile;
+// the activation and its gradient are formed on that way, from fp32.
+
+#include <algorithm>
 
 #include "gdr2_gatedff.hpp"
 #include "gdr2_bf16.hpp"
@@ -8,90 +24,407 @@ namespace gdr2 {
 
 namespace {
 
-constexpr int TM = 64, TK = 32, LK = TK + 4;  // tile, K step and LDS row stride (floats)
+constexpr int kCUs = 256;
+constexpr int STEP = 128;  // bytes of a row that one step takes
 
-__device__ __forceinline__ float ff_ld(const float* p) { return *p; }
-__device__ __forceinline__ float ff_ld(const bf16_t* p) { return __uint_as_float((uint32_t)p->x << 16); }
-__device__ __forceinline__ void ff_st(float* p, float x) { *p = x; }
-__device__ __forceinline__ void ff_st(bf16_t* p, float x) { *reinterpret_cast<__bf16*>(p) = (__bf16)x; }
-
-__device__ __forceinline__ void ff_act(int act, float g, float& a, float& slope) {
-  if (act == 0) {
-    const float s = 1.f / (1.f + expf(-g));
-    a = g * s;
-    slope = s * (1.f + g * (1.f - s));
-  } else {
-    const float s = 0.5f * (1.f + erff(g * 0.70710678118654752f));
-    a = g * s;
-    slope = s + g * expf(-0.5f * g * g) * 0.39894228040143268f;
+// 16 bytes of an operand: a bf16 fragment, or four fp32 ones
+template <typename T>
+struct FfType;
+template <>
+struct FfType<bf16_t> {
+  static constexpr int E = 2;
+  using Frag = bf8;
+  static __device__ __forceinline__ f4 mma(const Frag& a, const Frag& b, f4 c) { return gdr2::mma(a, b, c); }
+};
+template <>
+struct FfType<float> {
+  static constexpr int E = 4;
+  using Frag = f4;
+  static __device__ __forceinline__ f4 mma(const Frag& a, const Frag& b, f4 c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = mfma_f32(a[i], b[i], c);  // k = 4 (lane / 16) + i in both
+    return c;
   }
+};
+
+// ---- tiles in LDS -----------------------------------------------------------------------------
+// Rows: ROWS rows of 128 bytes, piece p of row r at place p ^ ff_row_swz(r).  16-byte reads serve 16 lanes
+// at a time: quads of rows {0-3, 8-11} or {4-7, 12-15}, two neighbouring pieces.
+__device__ __forceinline__ int ff_row_swz(int r) { return (r & 2) | ((r & 8) >> 1); }
+// Columns: STEP / E rows of ROWS elements.  bf16: the transposing load serves 32 lanes at a time, 32 bytes
+// of rows {0-3, 8-11} (+ 4); fp32: four rows, four apart, of 64 bytes.
+template <typename T>
+__device__ __forceinline__ int ff_col_swz(int k) {
+  return sizeof(T) == 2 ? ((k & 3) | ((k & 8) >> 1)) << 1 : (k >> 2 & 3) << 2;
+}
+
+// One operand's way into LDS: ROWS x 128 bytes by NW waves, 1 KB an instruction.
+template <typename T, bool COL, int ROWS, int NW>
+struct FfLoad {
+  static constexpr int NI = ROWS * STEP / 1024 / NW;             // instructions a wave
+  static constexpr int RB = COL ? ROWS * (int)sizeof(T) : STEP;  // bytes of an LDS row
+  static constexpr int RI = 1024 / RB;                           // LDS rows an instruction
+  // the exchange is the same in every instruction but for bit 3 of the row in fp32 columns
+  static constexpr int FLIP = COL && sizeof(T) == 4 ? (NW * RI & 8) : 0;
+  static_assert(NW * RI % 16 == 0 || FLIP != 0, "");
+  unsigned row;  // offset of the lane's row in the first instruction
+  int piece;     // and the lane's piece there
+  __device__ __forceinline__ FfLoad(unsigned ld, int lane, int wave) {  // ld: bytes from row to row
+    const int r = wave * RI + lane / (RB / 16);
+    piece = (lane % (RB / 16)) ^ (COL ? ff_col_swz<T>(r) : ff_row_swz(r));
+    row = r * ld;
+  }
+  __device__ __forceinline__ unsigned at(int i, unsigned ld) const {
+    return row + i * (NW * RI) * ld + ((piece ^ (i & 1 ? FLIP : 0)) << 4);
+  }
+};
+
+// Written out, and waited for by ff_landed: as builtins, the compiler would hold every LDS read
+// behind them.
+__device__ __forceinline__ void ff_to_lds(unsigned to, unsigned from, u4v buf) {
+  // m0, the place in LDS, has to be written a wait state before the load reads it
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(from), "s"(buf)
+               : "memory", "m0");
+}
+__device__ __forceinline__ void ff_landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ u4v ff_buffer(const void* p, int64_t left) {
+  const uint64_t at = (uint64_t)(uintptr_t)p;
+  const unsigned n = left <= 0 ? 0u : left > 0x7fffffff ? 0x7fffffffu : (unsigned)left;
+  return u4v{(unsigned)at, (unsigned)(at >> 32) & 0xffffu, n, 0x00020000u};
+}
+constexpr unsigned kOutside = 0x80000000u;  // an offset past every buffer
+
+}  // namespace
+
+template <typename T, int FORM, int END, int BM, int BN>
+struct FfTile {
+  static constexpr int E = sizeof(T);
+  static constexpr int NWM = BM / 64, NWN = 2, NW = NWM * NWN;  // waves of 64 x BN / 2
+  static constexpr int WN = BN / NWN, MT = 4, NT = WN / 16;
+  static constexpr int BK = STEP / E;
+  static constexpr bool ACOL = FORM == FF_COLUMNS, BCOL = FORM != FF_ROWS;
+  static constexpr int BUF = (BM + BN) * STEP;
+  static constexpr int SLD = WN + 4;                            // floats from row to row where C passes through LDS
+  static constexpr int BNC = END == FF_GATE ? BN / 2 : BN;      // columns of N that a tile takes
+};
+
+// A wave's 16 x WN strip of C, its fp32 values in LDS (s, rows of SLD floats): rows m.. of M, columns n.. of N.
+template <typename T, int FORM, int END, int BM, int BN>
+__device__ __forceinline__ void ff_strip(const FfArgs<T>& p, const float* s, int64_t m, int64_t n, int lane) {
+  using Z = FfTile<T, FORM, END, BM, BN>;
+  constexpr int COLS = END == FF_GATE ? Z::WN / 2 : Z::WN;  // of N
+  constexpr int LR = COLS / 4, RI = 64 / LR;                // lanes a row, rows at a time
+  const int c = 4 * (lane % LR);
+  const auto put = [&](T* to, const f4& x) {
+    if constexpr (sizeof(T) == 2)
+      st4(reinterpret_cast<__bf16*>(to), x[0], x[1], x[2], x[3]);
+    else
+      *reinterpret_cast<f4*>(to) = x;
+  };
+#pragma unroll 2
+  for (int r0 = 0; r0 < 16; r0 += RI) {
+    const int r = r0 + lane / LR;
+    const int64_t row = m + r, col = n + c;
+    if (row >= p.M || col >= p.N) continue;
+    const f4 x = *reinterpret_cast<const f4*>(s + r * Z::SLD + c);
+    if constexpr (END == FF_STORE) {
+      T* to = row < p.cut ? p.c[0] + row * p.N : p.c[1] + (row - p.cut) * p.N;
+      put(to + col, x);
+    } else {
+      const int64_t at = row * p.N + col;
+      f4 g, u, h, dg, du;
+      if constexpr (END == FF_GATE) {
+        g = x;
+        u = *reinterpret_cast<const f4*>(s + r * Z::SLD + COLS + c);
+        if (p.g) {
+          *reinterpret_cast<f4*>(p.g + at) = g;
+          *reinterpret_cast<f4*>(p.u + at) = u;
+        }
+        if (!p.h) continue;
+      } else {
+        g = *reinterpret_cast<const f4*>(p.g + at);
+        u = *reinterpret_cast<const f4*>(p.u + at);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float a, slope;
+        if (p.act == 0) {  // SiLU
+          const float sg = 1.f / (1.f + expf(-g[i]));
+          a = g[i] * sg;
+          slope = sg * (1.f + g[i] * (1.f - sg));
+        } else {  // GELU
+          const float sg = 0.5f * (1.f + erff(g[i] * 0.70710678118654752f));
+          a = g[i] * sg;
+          slope = END == FF_GRAD ? sg + g[i] * expf(-0.5f * g[i] * g[i]) * 0.39894228040143268f : 0.f;
+        }
+        h[i] = a * u[i];
+        if constexpr (END == FF_GRAD) {
+          dg[i] = x[i] * u[i] * slope;
+          du[i] = x[i] * a;
+        }
+      }
+      if (p.h) put(p.h + at, h);
+      if constexpr (END == FF_GRAD) {
+        put(p.dgu + row * 2 * p.N + col, dg);
+        put(p.dgu + row * 2 * p.N + p.N + col, du);
+      }
+    }
+  }
+}
+
+// What lanes of a wave leave for each other in LDS: it serves a wave's instructions in order.
+__device__ __forceinline__ void ff_wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// a strip's products, in the lanes' layout, through the wave's place in LDS
+template <typename T, int FORM, int END, int BM, int BN>
+__device__ __forceinline__ void ff_leave(const FfArgs<T>& p, const f4* x, float* s, int64_t m, int64_t n, int lane) {
+  using Z = FfTile<T, FORM, END, BM, BN>;
+  ff_wave_order();
+#pragma unroll
+  for (int j = 0; j < Z::NT; ++j) *reinterpret_cast<f4*>(s + (lane & 15) * Z::SLD + 16 * j + 4 * (lane >> 4)) = x[j];
+  ff_wave_order();
+  ff_strip<T, FORM, END, BM, BN>(p, s, m, n, lane);
+}
+
+// The tile of a workgroup: XCDs take blocks in turn, so that a run of neighbouring tiles, eight of M by
+// as many of N, is on one and shares its L2.
+__device__ __forceinline__ void ff_place(int t, int tiles, int tm, int tn, int& im, int& in) {
+  const int per = tiles / 8, rest = tiles % 8, x = t % 8;
+  t = x * per + min(x, rest) + t / 8;
+  constexpr int GM = 8;
+  const int group = t / (GM * tn), first = group * GM, rows = min(GM, tm - first), k = t - group * GM * tn;
+  im = first + k % rows;
+  in = k / rows;
+}
+
+template <typename T, int FORM, int END, int BM, int BN>
+__global__ __launch_bounds__(64 * (BM / 64) * 2, 2) void ff_kernel(FfArgs<T> p) {
+  using Z = FfTile<T, FORM, END, BM, BN>;
+  using F = FfType<T>;
+  using Frag = typename F::Frag;
+  constexpr int E = Z::E, MT = Z::MT, NT = Z::NT;
+  __shared__ __align__(1024) unsigned char smem[2 * Z::BUF];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / Z::NWN, wn = wave % Z::NWN, r16 = lane & 15, grp = lane >> 4;
+  const int tiles = p.tm * p.tn;
+  // whole tiles first; then parts of the others, a tile's parts apart
+  int t = blockIdx.x, part = 0, im, in;
+  if (t >= p.full) {
+    const int left = tiles - p.full;
+    part = (t - p.full) / left;
+    t = p.full + (t - p.full) % left;
+  }
+  const bool whole = t < p.full;
+  ff_place(t, tiles, p.tm, p.tn, im, in);
+  const int64_t m0 = (int64_t)im * BM, n0 = (int64_t)in * Z::BNC;
+  const int per = (int)((p.K + Z::BK - 1) / Z::BK), steps = per * p.pairs;  // steps of one product, of all
+  const int s0 = whole ? 0 : (int)((int64_t)steps * part / p.split);
+  const int s1 = whole ? steps : (int)((int64_t)steps * (part + 1) / p.split);
+
+  const unsigned la = (unsigned)(p.lda * E), lb = (unsigned)(p.ldb * E);
+  using LA = FfLoad<T, Z::ACOL, BM, Z::NW>;
+  using LB = FfLoad<T, Z::BCOL, BN, Z::NW>;
+  const LA fa(la, lane, wave);
+  const LB fb(lb, lane, wave);
+  const unsigned lds = (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void*)smem;
+  const auto fetch = [&](int s) {
+    const int pair = s >= per ? 1 : 0, k = s - pair * per;
+    const int64_t k0 = (int64_t)k * Z::BK;
+    const bool last = k == per - 1;
+    unsigned to = lds + (s & 1) * Z::BUF;
+    asm("" : "+s"(to));
+    {
+      const T* base = p.a + (pair ? p.a2 : 0);
+      const u4v buf = Z::ACOL ? ff_buffer(base + k0 * p.lda + m0, ((p.K - k0 - 1) * p.lda + p.M - m0) * E)
+                              : ff_buffer(base + m0 * p.lda + k0, ((min((int64_t)BM, p.M - m0) - 1) * p.lda + p.K - k0) * E);
+      const bool past = !Z::ACOL && last && k0 + fa.piece * (16 / E) >= p.K;
+#pragma unroll
+      for (int i = 0; i < LA::NI; ++i) ff_to_lds(to + (wave + i * Z::NW) * 1024, past ? kOutside : fa.at(i, la), buf);
+    }
+    {
+      const bool past = !Z::BCOL && last && k0 + fb.piece * (16 / E) >= p.K;
+      to += BM * STEP;
+      if constexpr (END == FF_GATE) {
+        // the tile's rows: for each wave column half of them Wg's, half Wu's, of the same channels
+        constexpr int HALF = Z::WN / 2;
+        const int64_t left = ((min((int64_t)Z::BNC, p.N - n0) - 1) * p.ldb + p.K - k0) * E;
+        const u4v b0 = ff_buffer(p.b[0] + n0 * p.ldb + k0, left), b1 = ff_buffer(p.b[1] + n0 * p.ldb + k0, left);
+#pragma unroll
+        for (int i = 0; i < LB::NI; ++i) {
+          const int row = (wave + i * Z::NW) * LB::RI, w = row % Z::WN, f = row / Z::WN * HALF + w % HALF;  // the instruction's first row
+          const unsigned at = past ? kOutside : (f + lane / 8) * lb + fb.piece * 16;
+          if (w < HALF)
+            ff_to_lds(to + (wave + i * Z::NW) * 1024, at, b0);
+          else
+            ff_to_lds(to + (wave + i * Z::NW) * 1024, at, b1);
+        }
+      } else {
+        const T* base = p.b[pair];
+        const u4v buf = Z::BCOL ? ff_buffer(base + k0 * p.ldb + n0, ((p.K - k0 - 1) * p.ldb + p.N - n0) * E)
+                                : ff_buffer(base + n0 * p.ldb + k0, ((min((int64_t)BN, p.N - n0) - 1) * p.ldb + p.K - k0) * E);
+#pragma unroll
+        for (int i = 0; i < LB::NI; ++i) ff_to_lds(to + (wave + i * Z::NW) * 1024, past ? kOutside : fb.at(i, lb), buf);
+      }
+    }
+  };
+  // fragment of 16 rows (of M or N) from r0, half ks of the step
+  const auto rows_frag = [&](const unsigned char* s, int r0, int ks) {
+    return *reinterpret_cast<const Frag*>(s + (r0 + r16) * STEP + (((4 * ks + grp) ^ ff_row_swz(r16)) << 4));
+  };
+  const auto cols_frag = [&](const unsigned char* s, int rb, int r0, int ks) {
+    Frag x;
+    if constexpr (E == 2) {
+      const int k = 32 * ks + 8 * grp + (r16 >> 2);
+      const unsigned char* q = s + k * rb + (((2 * (r0 / 16)) ^ ff_col_swz<T>(k)) << 4) + 8 * (r16 & 3);
+      x = ld_tr8p(reinterpret_cast<const __bf16*>(q), reinterpret_cast<const __bf16*>(q + 4 * rb));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int k = 16 * ks + 4 * grp + i;
+        x[i] = *reinterpret_cast<const float*>(s + k * rb + (((r0 / 4) ^ ff_col_swz<T>(k)) << 4) + 4 * r16);
+      }
+    }
+    return x;
+  };
+  f4 acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = f4zero();
+  if (s0 < s1) fetch(s0);
+  for (int s = s0; s < s1; ++s) {
+    ff_landed();
+    __syncthreads();
+    if (s + 1 < s1) fetch(s + 1);
+    const unsigned char *sa = smem + (s & 1) * Z::BUF, *sb = sa + BM * STEP;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      Frag a[MT], b[NT];
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+        a[i] = Z::ACOL ? cols_frag(sa, BM * E, 64 * wm + 16 * i, ks) : rows_frag(sa, 64 * wm + 16 * i, ks);
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+        b[j] = Z::BCOL ? cols_frag(sb, BN * E, Z::WN * wn + 16 * j, ks) : rows_frag(sb, Z::WN * wn + 16 * j, ks);
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = F::mma(b[j], a[i], acc[i][j]);
+    }
+  }
+  if (!whole) {  // the lanes' registers as they are: 16 bytes a lane and instruction
+    const int64_t slot = (int64_t)(t - p.full) * p.split + part;
+    float* to = p.part + slot * (BM * BN) + wave * (64 * Z::WN) + 4 * lane;
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) *reinterpret_cast<f4*>(to + (i * NT + j) * 256) = acc[i][j];
+    return;
+  }
+  ff_landed();  // (nothing is under way; said where a path from a load to the barrier is looked for)
+  __syncthreads();
+  float* stage = reinterpret_cast<float*>(smem) + wave * (16 * Z::SLD);
+  const int64_t n = n0 + (END == FF_GATE ? Z::WN / 2 : Z::WN) * wn;
+#pragma unroll
+  for (int i = 0; i < MT; ++i) ff_leave<T, FORM, END, BM, BN>(p, acc[i], stage, m0 + 64 * wm + 16 * i, n, lane);
+}
+
+// The parts of the tiles that were cut, a strip a wave
+template <typename T, int FORM, int END, int BM, int BN>
+__global__ __launch_bounds__(256) void ff_join_kernel(FfArgs<T> p) {
+  using Z = FfTile<T, FORM, END, BM, BN>;
+  constexpr int STRIPS = Z::NW * Z::MT;
+  __shared__ __align__(16) float stage[4][16 * Z::SLD];
+  const int lane = threadIdx.x & 63, w4 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int q = blockIdx.x * 4 + w4, tile = q / STRIPS, strip = q % STRIPS, wave = strip / Z::MT, i = strip % Z::MT;
+  int im, in;
+  ff_place(p.full + tile, p.tm * p.tn, p.tm, p.tn, im, in);
+  f4 x[Z::NT];
+  const float* from = p.part + (int64_t)tile * p.split * (BM * BN) + wave * (64 * Z::WN) + i * Z::NT * 256 + 4 * lane;
+#pragma unroll
+  for (int j = 0; j < Z::NT; ++j) x[j] = *reinterpret_cast<const f4*>(from + j * 256);
+  for (int s = 1; s < p.split; ++s) {
+    from += BM * BN;
+#pragma unroll
+    for (int j = 0; j < Z::NT; ++j) x[j] += *reinterpret_cast<const f4*>(from + j * 256);
+  }
+  const int64_t m = (int64_t)im * BM + 64 * (wave / Z::NWN) + 16 * i;
+  const int64_t n = (int64_t)in * Z::BNC + (END == FF_GATE ? Z::WN / 2 : Z::WN) * (wave % Z::NWN);
+  ff_leave<T, FORM, END, BM, BN>(p, x, stage[w4], m, n, lane);
+}
+
+namespace {
+
+struct FfPlan {
+  int bm, bn, tm, tn, full, split, slots;
+};
+FfPlan ff_plan(int end, int64_t M, int64_t N, int64_t K, int pairs, int E, bool large) {
+  FfPlan q{};
+  q.bm = q.bn = large ? 256 : 128;
+  q.slots = large ? kCUs : 2 * kCUs;
+  const int bnc = end == FF_GATE ? q.bn / 2 : q.bn;
+  q.tm = (int)((M + q.bm - 1) / q.bm);
+  q.tn = (int)((N + bnc - 1) / bnc);
+  const int64_t tiles = (int64_t)q.tm * q.tn, steps = (K + STEP / E - 1) / (STEP / E) * pairs;
+  q.full = (int)(tiles / q.slots * q.slots);
+  const int64_t left = tiles - q.full;
+  q.split = 1;
+  if (left > 0) q.split = (int)std::max<int64_t>(1, std::min<int64_t>(q.slots / left, steps / 4));
+  if (q.split == 1) q.full = (int)tiles;
+  return q;
+}
+// 256 x 256 tiles where they give every CU one
+FfPlan ff_choose(int end, int64_t M, int64_t N, int64_t K, int pairs, int E) {
+  const FfPlan large = ff_plan(end, M, N, K, pairs, E, true);
+  if (E == 2 && (int64_t)large.tm * large.tn >= kCUs) return large;
+  return ff_plan(end, M, N, K, pairs, E, false);
+}
+
+template <typename T, int FORM, int END, int BM>
+hipError_t ff_go(const FfArgs<T>& a, hipStream_t st) {
+  const int left = a.tm * a.tn - a.full;
+  hipLaunchKernelGGL((ff_kernel<T, FORM, END, BM, BM>), dim3((unsigned)(a.full + left * a.split)), dim3(64 * (BM / 64) * 2), 0, st, a);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && left > 0) {
+    using Z = FfTile<T, FORM, END, BM, BM>;
+    hipLaunchKernelGGL((ff_join_kernel<T, FORM, END, BM, BM>), dim3((unsigned)(left * (Z::NW * Z::MT / 4))), dim3(256), 0, st, a);
+    e = hipGetLastError();
+  }
+  return e;
 }
 
 }  // namespace
 
-// A 64 x 64 tile a workgroup, a 16 x 64 strip a wave.
-template <typename T, typename TC>
-__global__ __launch_bounds__(256) void ff_gemm_kernel(FfGemmArgs<T, TC> p) {
-  __shared__ float sa[TM * LK], sb[TM * LK];
-  const int64_t nt = (p.N + TM - 1) / TM, m0 = blockIdx.x / nt * TM, n0 = blockIdx.x % nt * TM;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  f4 acc[4] = {f4zero(), f4zero(), f4zero(), f4zero()};
-  for (int q = 0; q < p.pairs; ++q)
-    for (int64_t k0 = 0; k0 < p.K; k0 += TK) {
-      __syncthreads();
-      for (int e = tid; e < TM * TK; e += 256) {
-        const int r = e / TK, k = e % TK;
-        const bool in = k0 + k < p.K;
-        sa[r * LK + k] = in && m0 + r < p.M ? ff_ld(p.a[q] + (m0 + r) * p.am + (k0 + k) * p.ak) : 0.f;
-        sb[r * LK + k] = in && n0 + r < p.N ? ff_ld(p.b[q] + (n0 + r) * p.bn + (k0 + k) * p.bk) : 0.f;
-      }
-      __syncthreads();
-#pragma unroll
-      for (int k = 0; k < TK; k += 4) {
-        const float x = sa[(16 * wave + (lane & 15)) * LK + k + (lane >> 4)];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[j] = mfma_f32(x, sb[(16 * j + (lane & 15)) * LK + k + (lane >> 4)], acc[j]);
-      }
-    }
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int64_t m = m0 + 16 * wave + 4 * (lane >> 4) + u, n = n0 + 16 * j + (lane & 15);
-      if (m < p.M && n < p.N) ff_st(p.c + m * p.N + n, acc[j][u]);
-    }
+template <typename T>
+size_t ff_part_bytes(int form, int end, int64_t M, int64_t N, int64_t K, int pairs) {
+  const FfPlan q = ff_choose(end, M, N, K, pairs, sizeof(T));
+  return (size_t)((int64_t)q.tm * q.tn - q.full) * q.split * q.bm * q.bn * 4;
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void ff_act_kernel(FfActArgs<T> p) {
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (e >= p.n) return;
-  const float u = p.u[e];
-  float a, slope;
-  ff_act(p.act, p.g[e], a, slope);
-  ff_st(p.h + e, a * u);
-  if (p.dh) {
-    const float d = p.dh[e];
-    ff_st(p.dg + e, d * u * slope);
-    ff_st(p.du + e, d * a);
-  }
+template <typename T, int FORM, int END>
+hipError_t launch_ff(FfArgs<T> a, hipStream_t st) {
+  const FfPlan q = ff_choose(END, a.M, a.N, a.K, a.pairs, sizeof(T));
+  a.tm = q.tm;
+  a.tn = q.tn;
+  a.full = q.full;
+  a.split = q.split;
+  if constexpr (sizeof(T) == 2)
+    if (q.bm == 256) return ff_go<T, FORM, END, 256>(a, st);
+  return ff_go<T, FORM, END, 128>(a, st);
 }
 
-template <typename T, typename TC>
-hipError_t launch_ff_gemm(const FfGemmArgs<T, TC>& a, hipStream_t st) {
-  const int64_t blocks = ((a.M + TM - 1) / TM) * ((a.N + TM - 1) / TM);
-  hipLaunchKernelGGL((ff_gemm_kernel<T, TC>), dim3((unsigned)blocks), dim3(256), 0, st, a);
-  return hipGetLastError();
-}
-template <typename T>
-hipError_t launch_ff_act(const FfActArgs<T>& a, hipStream_t st) {
-  hipLaunchKernelGGL(ff_act_kernel<T>, dim3((unsigned)((a.n + 255) / 256)), dim3(256), 0, st, a);
-  return hipGetLastError();
-}
-template hipError_t launch_ff_gemm<float, float>(const FfGemmArgs<float, float>&, hipStream_t);
-template hipError_t launch_ff_gemm<bf16_t, float>(const FfGemmArgs<bf16_t, float>&, hipStream_t);
-template hipError_t launch_ff_gemm<bf16_t, bf16_t>(const FfGemmArgs<bf16_t, bf16_t>&, hipStream_t);
-template hipError_t launch_ff_act<float>(const FfActArgs<float>&, hipStream_t);
-template hipError_t launch_ff_act<bf16_t>(const FfActArgs<bf16_t>&, hipStream_t);
+#define GDR2_FF(T)                                                        \
+  template size_t ff_part_bytes<T>(int, int, int64_t, int64_t, int64_t, int);   \
+  template hipError_t launch_ff<T, FF_ROWS, FF_STORE>(FfArgs<T>, hipStream_t);    \
+  template hipError_t launch_ff<T, FF_ROWS, FF_GATE>(FfArgs<T>, hipStream_t);     \
+  template hipError_t launch_ff<T, FF_MIXED, FF_STORE>(FfArgs<T>, hipStream_t);   \
+  template hipError_t launch_ff<T, FF_MIXED, FF_GRAD>(FfArgs<T>, hipStream_t);    \
+  template hipError_t launch_ff<T, FF_COLUMNS, FF_STORE>(FfArgs<T>, hipStream_t);
+GDR2_FF(float)
+GDR2_FF(bf16_t)
 
 }  // namespace gdr2

@@ -6,28 +6,40 @@
 
 namespace gdr2 {
 
-// C (M x N) = sum over operand pairs of A B^T, fp32 accumulation:
-//   A's element (m, k) at a[m * am + k * ak], B's element (n, k) at b[n * bn + k * bk].
-template <typename T, typename TC>
-struct FfGemmArgs {
-  const T *a[2], *b[2];
-  int64_t am, ak, bn, bk;
-  int pairs;
-  TC* c;
+// Products C = A B, A (M, K), B (K, N), fp32 accumulation.  An operand lies with its sum along the rows
+// of memory ("rows") or across them ("columns"):
+//     FF_ROWS     A (M, K), B^T (N, K)     x Wg^T, x Wu^T, h Wd^T
+//     FF_MIXED    A (M, K), B (K, N)       dy Wd, dg Wg + du Wu
+//     FF_COLUMNS  A^T (K, M), B (K, N)     dg^T x, du^T x, dy^T h
+enum FfForm : int { FF_ROWS = 0, FF_MIXED = 1, FF_COLUMNS = 2 };
+// What becomes of C:
+//     FF_STORE  rounded and stored
+//     FF_GATE   B is a pair, C a pair g, u: h = act(g) u, and g, u themselves where asked for
+//     FF_GRAD   C is dh: h, dg and du from it and the stored g, u
+enum FfEnd : int { FF_STORE = 0, FF_GATE = 1, FF_GRAD = 2 };
+
+template <typename T>
+struct FfArgs {
+  const T *a, *b[2];
+  int64_t lda, ldb;   // elements from one row of memory to the next
   int64_t M, N, K;
-};
-
-template <typename T>
-struct FfActArgs {
-  const float *g, *u, *dh;  // dh NULL: forward
-  T *h, *dg, *du;
-  int64_t n;
+  int64_t a2;         // pairs == 2: the second product's A starts a2 elements further; its B is b[1]
+  int pairs;
+  T* c[2];            // FF_STORE: rows from `cut` on are those of c[1]
+  int64_t cut;
+  float *g, *u;       // (M, N); FF_GATE: nullable; FF_GRAD: read
+  T *h, *dgu;         // h (M, N), nullable; dg, du side by side (M, 2 N)
   int act;
+  // set by the launch
+  float* part;        // partial tiles
+  int tm, tn;         // tiles
+  int full, split;    // tiles computed whole; parts of every other one
 };
 
-template <typename T, typename TC>
-hipError_t launch_ff_gemm(const FfGemmArgs<T, TC>& a, hipStream_t st);
+// Bytes of partial tiles that a call with these arguments takes.
 template <typename T>
-hipError_t launch_ff_act(const FfActArgs<T>& a, hipStream_t st);
+size_t ff_part_bytes(int form, int end, int64_t M, int64_t N, int64_t K, int pairs);
+template <typename T, int FORM, int END>
+hipError_t launch_ff(FfArgs<T> a, hipStream_t st);
 
 }  // namespace gdr2

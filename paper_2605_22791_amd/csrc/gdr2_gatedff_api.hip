@@ -3,6 +3,8 @@
 
 #include "../../include/gdr2_gatedff.h"
 
+#include <algorithm>
+
 #include "gdr2_gatedff.hpp"
 #include "gdr2_host.hpp"
 
@@ -23,13 +25,34 @@ gdr2_status ff_check(const gdr2_gatedff* p) {
   return GDR2_OK;
 }
 
-// fp32 g and u (rows, F), first: what a saving forward leaves; h (rows, F); backward also dh in
-// fp32, and the gradients at g and u
+// The six products of the block, by what they take
+template <typename T>
+FfArgs<T> ff_args(int64_t M, int64_t N, int64_t K, const void* a, int64_t lda, const void* b0, const void* b1, int64_t ldb,
+                  void* part) {
+  FfArgs<T> p{};
+  p.a = static_cast<const T*>(a);
+  p.b[0] = static_cast<const T*>(b0);
+  p.b[1] = static_cast<const T*>(b1);
+  p.lda = lda;
+  p.ldb = ldb;
+  p.M = M;
+  p.N = N;
+  p.K = K;
+  p.pairs = 1;
+  p.cut = M;
+  p.part = static_cast<float*>(part);
+  return p;
+}
+
+// fp32 g and u (rows, F), first: what a saving forward leaves; h (rows, F); backward also the
+// gradients at g and u (rows, 2 F); partial tiles of the products
 struct FfLayout {
-  size_t g, u, h, dh, dg, du, total;
+  size_t g, u, h, dgu, part, total;
 };
-FfLayout ff_layout(const gdr2_gatedff* p, bool bwd) {
-  const size_t n = (size_t)p->rows * p->F, e = p->dtype == GDR2_BF16 ? 2 : 4;
+template <typename T>
+FfLayout ff_layout_of(const gdr2_gatedff* p, bool bwd) {
+  const int64_t M = p->rows, D = p->D, F = p->F;
+  const size_t n = (size_t)M * F, e = sizeof(T);
   FfLayout L{};
   size_t off = 0;
   const auto take = [&](size_t bytes) {
@@ -37,33 +60,44 @@ FfLayout ff_layout(const gdr2_gatedff* p, bool bwd) {
     off += round_up(bytes);
     return at;
   };
-  L.g = take(4 * n);
-  L.u = take(4 * n);
-  L.h = take(e * n);
   if (bwd) {
-    L.dh = take(4 * n);
-    L.dg = take(e * n);
-    L.du = take(e * n);
+    L.g = take(4 * n);
+    L.u = take(4 * n);
   }
+  L.h = take(e * n);
+  if (bwd) L.dgu = take(2 * e * n);
+  size_t part = 0;
+  const auto product = [&](int form, int end, int64_t M, int64_t N, int64_t K, int pairs) {
+    part = std::max(part, ff_part_bytes<T>(form, end, M, N, K, pairs));
+  };
+  if (M > 0) {
+    product(FF_ROWS, FF_GATE, M, F, D, 1);
+    product(FF_ROWS, FF_STORE, M, D, F, 1);
+    if (bwd) {
+      product(FF_MIXED, FF_GRAD, M, F, D, 1);
+      product(FF_MIXED, FF_STORE, M, D, F, 2);
+      product(FF_COLUMNS, FF_STORE, 2 * F, D, M, 1);
+      product(FF_COLUMNS, FF_STORE, D, F, M, 1);
+    }
+  }
+  L.part = take(part);
   L.total = off + kAlign;
   return L;
 }
+FfLayout ff_layout(const gdr2_gatedff* p, bool bwd) {
+  return p->dtype == GDR2_FP32 ? ff_layout_of<float>(p, bwd) : ff_layout_of<bf16_t>(p, bwd);
+}
 
-// c (M, N) = a b^T with rows of a and b along the products' sum
-template <typename T, typename TC>
-hipError_t rows_by_rows(const T* a, const T* b, TC* c, int64_t M, int64_t N, int64_t K, hipStream_t st) {
-  return launch_ff_gemm<T, TC>({{a, nullptr}, {b, nullptr}, K, 1, K, 1, 1, c, M, N, K}, st);
-}
-// c (M, N) = a0 b0 + a1 b1, a (M, K), b (K, N); a1 may be NULL
-template <typename T, typename TC>
-hipError_t rows_by_columns(const T* a0, const T* b0, const T* a1, const T* b1, TC* c, int64_t M, int64_t N, int64_t K,
-                           hipStream_t st) {
-  return launch_ff_gemm<T, TC>({{a0, a1}, {b0, b1}, K, 1, 1, N, a1 ? 2 : 1, c, M, N, K}, st);
-}
-// c (M, N) = a^T b, a (K, M), b (K, N)
+// h and, where they are asked for, g and u
 template <typename T>
-hipError_t columns_by_columns(const T* a, const T* b, T* c, int64_t M, int64_t N, int64_t K, hipStream_t st) {
-  return launch_ff_gemm<T, T>({{a, nullptr}, {b, nullptr}, 1, M, 1, N, 1, c, M, N, K}, st);
+hipError_t ff_gate(const gdr2_gatedff* p, const void* x, const void* Wg, const void* Wu, float* g, float* u, T* h, void* part,
+                   hipStream_t st) {
+  FfArgs<T> a = ff_args<T>(p->rows, p->F, p->D, x, p->D, Wg, Wu, p->D, part);
+  a.g = g;
+  a.u = u;
+  a.h = h;
+  a.act = p->act;
+  return launch_ff<T, FF_ROWS, FF_GATE>(a, st);
 }
 
 }  // namespace
@@ -89,16 +123,13 @@ gdr2_status gdr2_gatedff_fwd(const gdr2_gatedff* p, const void* x, const void* W
   if (p->rows == 0) return GDR2_OK;
   const auto run = [&](auto t) {
     using T = decltype(t);
-    const T *xs = static_cast<const T*>(x), *wg = static_cast<const T*>(Wg), *wu = static_cast<const T*>(Wu);
-    const int64_t M = p->rows, D = p->D, F = p->F;
-    hipError_t e = rows_by_rows<T, float>(xs, wg, at<float>(ws, L.g), M, F, D, stream);
-    if (e == hipSuccess) e = rows_by_rows<T, float>(xs, wu, at<float>(ws, L.u), M, F, D, stream);
-    if (e == hipSuccess)
-      e = launch_ff_act<T>({at<float>(ws, L.g), at<float>(ws, L.u), nullptr, at<T>(ws, L.h), nullptr, nullptr, M * F, p->act},
-                           stream);
-    if (e == hipSuccess)
-      e = rows_by_rows<T, T>(at<T>(ws, L.h), static_cast<const T*>(Wd), static_cast<T*>(y), M, D, F, stream);
-    return e;
+    T* h = at<T>(ws, L.h);
+    void* part = at<char>(ws, L.part);
+    hipError_t e = ff_gate<T>(p, x, Wg, Wu, save ? at<float>(ws, L.g) : nullptr, save ? at<float>(ws, L.u) : nullptr, h, part, stream);
+    if (e != hipSuccess) return e;
+    FfArgs<T> a = ff_args<T>(p->rows, p->D, p->F, h, p->F, Wd, nullptr, p->F, part);
+    a.c[0] = static_cast<T*>(y);
+    return launch_ff<T, FF_ROWS, FF_STORE>(a, stream);
   };
   return hip_status(p->dtype == GDR2_FP32 ? run(0.f) : run(bf16_t{}), stream);
 }
@@ -118,25 +149,39 @@ gdr2_status gdr2_gatedff_bwd(const gdr2_gatedff* p, const void* x, const void* W
   if (ws_bytes < L.total) return GDR2_EWORKSPACE;
   const auto run = [&](auto t) {
     using T = decltype(t);
-    const T *xs = static_cast<const T*>(x), *wg = static_cast<const T*>(Wg), *wu = static_cast<const T*>(Wu);
-    const T *wd = static_cast<const T*>(Wd), *d = static_cast<const T*>(dy);
-    float *g = at<float>(ws, L.g), *u = at<float>(ws, L.u), *dh = at<float>(ws, L.dh);
-    T *h = at<T>(ws, L.h), *dg = at<T>(ws, L.dg), *du = at<T>(ws, L.du);
+    float *g = at<float>(ws, L.g), *u = at<float>(ws, L.u);
+    T *h = at<T>(ws, L.h), *dgu = at<T>(ws, L.dgu);
+    void* part = at<char>(ws, L.part);
     const int64_t M = p->rows, D = p->D, F = p->F;
     hipError_t e = hipSuccess;
     if (M > 0) {
-      if (!saved) {
-        e = rows_by_rows<T, float>(xs, wg, g, M, F, D, stream);
-        if (e == hipSuccess) e = rows_by_rows<T, float>(xs, wu, u, M, F, D, stream);
+      if (!saved) e = ff_gate<T>(p, x, Wg, Wu, g, u, nullptr, part, stream);
+      if (e != hipSuccess) return e;
+      FfArgs<T> a = ff_args<T>(M, F, D, dy, D, Wd, nullptr, F, part);
+      a.g = g;
+      a.u = u;
+      a.h = weights ? h : nullptr;
+      a.dgu = dgu;
+      a.act = p->act;
+      e = launch_ff<T, FF_MIXED, FF_GRAD>(a, stream);
+      if (e == hipSuccess && dx) {
+        FfArgs<T> b = ff_args<T>(M, D, F, dgu, 2 * F, Wg, Wu, D, part);
+        b.pairs = 2;
+        b.a2 = F;
+        b.c[0] = static_cast<T*>(dx);
+        e = launch_ff<T, FF_MIXED, FF_STORE>(b, stream);
       }
-      if (e == hipSuccess) e = rows_by_columns<T, float>(d, wd, nullptr, nullptr, dh, M, F, D, stream);
-      if (e == hipSuccess) e = launch_ff_act<T>({g, u, dh, h, dg, du, M * F, p->act}, stream);
-      if (e == hipSuccess && dx) e = rows_by_columns<T, T>(dg, wg, du, wu, static_cast<T*>(dx), M, D, F, stream);
     }
     if (e == hipSuccess && weights) {  // no row: zero
-      e = columns_by_columns<T>(dg, xs, static_cast<T*>(dWg), F, D, M, stream);
-      if (e == hipSuccess) e = columns_by_columns<T>(du, xs, static_cast<T*>(dWu), F, D, M, stream);
-      if (e == hipSuccess) e = columns_by_columns<T>(d, h, static_cast<T*>(dWd), D, F, M, stream);
+      FfArgs<T> a = ff_args<T>(2 * F, D, M, dgu, 2 * F, x, nullptr, D, part);
+      a.c[0] = static_cast<T*>(dWg);
+      a.c[1] = static_cast<T*>(dWu);
+      a.cut = F;
+      e = launch_ff<T, FF_COLUMNS, FF_STORE>(a, stream);
+      if (e != hipSuccess) return e;
+      FfArgs<T> b = ff_args<T>(D, F, M, dy, D, h, nullptr, F, part);
+      b.c[0] = static_cast<T*>(dWd);
+      e = launch_ff<T, FF_COLUMNS, FF_STORE>(b, stream);
     }
     return e;
   };
