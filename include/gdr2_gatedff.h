@@ -14,7 +14,8 @@
  * D and F are multiples of 8 up to 65536, else GDR2_EUNSUPPORTED; rows from 0 to 2^24 (0 is
  * GDR2_OK: the forward does nothing, the backward sets the gradients of the weights to zero).
  * Products accumulate in fp32.  bf16 problems round h, and backward the gradients at g and u, to
- * bf16 once on their way into the products that read them, from fp32 values of g and u.
+ * bf16 once on their way into the products that read them; the backward reads g and u in 11 bits of
+ * their own (a power of two for each row and 32 channels beside them), whether saved or formed again.
  *
  * Errors, ownership, streams and GDR2_DEBUG_SYNC as in gdr2.h.  The same call gives the same bits.
  */
@@ -40,13 +41,13 @@ typedef struct gdr2_gatedff {
  * save = 1). */
 gdr2_status gdr2_gatedff_workspace_bytes(const gdr2_gatedff* problem, int for_backward, size_t* bytes);
 
-/* Forward.  save = 1 leaves g and u in ws (sized for the backward), in fp32. */
+/* Forward.  save = 1 leaves g, u and h in ws (sized for the backward). */
 gdr2_status gdr2_gatedff_fwd(const gdr2_gatedff* problem, const void* x, const void* Wg, const void* Wu, const void* Wd,
                              void* y, void* ws, size_t ws_bytes, int save, hipStream_t stream);
 
 /* Gradients of sum <y, dy>.  dx may be NULL (not wanted), and so may dWg, dWu and dWd together
- * (frozen weights); not all four.  saved = 1 takes g and u that a save = 1 forward with the same
- * problem, x, Wg and Wu left in ws, and leaves them there; saved = 0 forms them again. */
+ * (frozen weights); not all four.  saved = 1 takes what a save = 1 forward with the same
+ * problem, x, Wg and Wu left in ws, and leaves it there; saved = 0 forms it again. */
 gdr2_status gdr2_gatedff_bwd(const gdr2_gatedff* problem, const void* x, const void* Wg, const void* Wu, const void* Wd,
                              const void* dy, void* dx, void* dWg, void* dWu, void* dWd, void* ws, size_t ws_bytes,
                              int saved, hipStream_t stream);

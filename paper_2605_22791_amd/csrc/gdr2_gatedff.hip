@@ -108,67 +108,87 @@ struct FfTile {
   static constexpr int BNC = END == FF_GATE ? BN / 2 : BN;      // columns of N that a tile takes
 };
 
-// A wave's 16 x WN strip of C, its fp32 values in LDS (s, rows of SLD floats): rows m.. of M, columns n.. of N.
+// A wave's strip of C: 16 rows x WN columns, COLS of N; through LDS a lane has four neighbouring columns
+// of IT rows, RI apart.
 template <typename T, int FORM, int END, int BM, int BN>
-__device__ __forceinline__ void ff_strip(const FfArgs<T>& p, const float* s, int64_t m, int64_t n, int lane) {
+struct FfStrip : FfTile<T, FORM, END, BM, BN> {
   using Z = FfTile<T, FORM, END, BM, BN>;
-  constexpr int COLS = END == FF_GATE ? Z::WN / 2 : Z::WN;  // of N
-  constexpr int LR = COLS / 4, RI = 64 / LR;                // lanes a row, rows at a time
-  const int c = 4 * (lane % LR);
-  const auto put = [&](T* to, const f4& x) {
-    if constexpr (sizeof(T) == 2)
-      st4(reinterpret_cast<__bf16*>(to), x[0], x[1], x[2], x[3]);
-    else
-      *reinterpret_cast<f4*>(to) = x;
-  };
-#pragma unroll 2
-  for (int r0 = 0; r0 < 16; r0 += RI) {
-    const int r = r0 + lane / LR;
-    const int64_t row = m + r, col = n + c;
-    if (row >= p.M || col >= p.N) continue;
-    const f4 x = *reinterpret_cast<const f4*>(s + r * Z::SLD + c);
-    if constexpr (END == FF_STORE) {
-      T* to = row < p.cut ? p.c[0] + row * p.N : p.c[1] + (row - p.cut) * p.N;
-      put(to + col, x);
-    } else {
-      const int64_t at = row * p.N + col;
-      f4 g, u, h, dg, du;
-      if constexpr (END == FF_GATE) {
-        g = x;
-        u = *reinterpret_cast<const f4*>(s + r * Z::SLD + COLS + c);
-        if (p.g) {
-          *reinterpret_cast<f4*>(p.g + at) = g;
-          *reinterpret_cast<f4*>(p.u + at) = u;
-        }
-        if (!p.h) continue;
-      } else {
-        g = *reinterpret_cast<const f4*>(p.g + at);
-        u = *reinterpret_cast<const f4*>(p.u + at);
-      }
+  static constexpr int COLS = END == FF_GATE ? Z::WN / 2 : Z::WN, LR = COLS / 4, RI = 64 / LR, IT = 16 / RI;
+  static constexpr bool HALVES = END == FF_GATE && sizeof(T) == 2;
+  static constexpr int NB = Z::WN / kFfBlock;                  // blocks of a row of the strip with a power of their own
+  static constexpr int BYTES = 16 * (Z::SLD + (HALVES ? NB : 0)) * 4;  // LDS of a wave
+  int64_t m, n;  // the strip's first row and column
+  int r, c;      // the lane's first row and its columns, within the strip
+  __device__ __forceinline__ FfStrip(int64_t m, int64_t n, int lane) : m(m), n(n), r(lane / LR), c(4 * (lane % LR)) {}
+  // the lane's rows that there are, RI apart
+  __device__ __forceinline__ int rows(const FfArgs<T>& p) const {
+    const int left = (int)min((int64_t)16, p.M - m) - r;
+    return n + c < p.N && left > 0 ? (left + RI - 1) / RI : 0;
+  }
+};
+
+// The stored g and u of a strip, loaded ahead
+template <typename T, class S>
+struct FfPast {
+  f4 g[S::IT], u[S::IT];
+  __device__ __forceinline__ void load(const FfArgs<T>& p, const S& s) {
+    const int rows = s.rows(p);
+    const int64_t at = (s.m + s.r) * p.N + s.n + s.c;
+    const float *gp = static_cast<const float*>(p.hid.g) + at, *up = static_cast<const float*>(p.hid.u) + at;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float a, slope;
-        if (p.act == 0) {  // SiLU
-          const float sg = 1.f / (1.f + expf(-g[i]));
-          a = g[i] * sg;
-          slope = sg * (1.f + g[i] * (1.f - sg));
-        } else {  // GELU
-          const float sg = 0.5f * (1.f + erff(g[i] * 0.70710678118654752f));
-          a = g[i] * sg;
-          slope = END == FF_GRAD ? sg + g[i] * expf(-0.5f * g[i] * g[i]) * 0.39894228040143268f : 0.f;
-        }
-        h[i] = a * u[i];
-        if constexpr (END == FF_GRAD) {
-          dg[i] = x[i] * u[i] * slope;
-          du[i] = x[i] * a;
-        }
+    for (int it = 0; it < S::IT; ++it, gp += S::RI * p.N, up += S::RI * p.N)
+      if (it < rows) {
+        g[it] = *reinterpret_cast<const f4*>(gp);
+        u[it] = *reinterpret_cast<const f4*>(up);
       }
-      if (p.h) put(p.h + at, h);
-      if constexpr (END == FF_GRAD) {
-        put(p.dgu + row * 2 * p.N + col, dg);
-        put(p.dgu + row * 2 * p.N + p.N + col, du);
+  }
+  __device__ __forceinline__ void get(int it, f4& gx, f4& ux) const { gx = g[it], ux = u[it]; }
+};
+template <class S>
+struct FfPast<bf16_t, S> {
+  f16x4 g[S::IT], u[S::IT];
+  int8_t ge[S::IT], ue[S::IT];
+  __device__ __forceinline__ void load(const FfArgs<bf16_t>& p, const S& s) {
+    const int rows = s.rows(p);
+    const int64_t nb = (p.N + kFfBlock - 1) / kFfBlock, at = (s.m + s.r) * p.N + s.n + s.c;
+    const _Float16 *gp = static_cast<const _Float16*>(p.hid.g) + at, *up = static_cast<const _Float16*>(p.hid.u) + at;
+    int64_t b = (s.m + s.r) * nb + (s.n + s.c) / kFfBlock;
+#pragma unroll
+    for (int it = 0; it < S::IT; ++it, gp += S::RI * p.N, up += S::RI * p.N, b += S::RI * nb)
+      if (it < rows) {
+        g[it] = *reinterpret_cast<const f16x4*>(gp);
+        u[it] = *reinterpret_cast<const f16x4*>(up);
+        ge[it] = p.hid.ge[b];
+        ue[it] = p.hid.ue[b];
       }
-    }
+  }
+  __device__ __forceinline__ void get(int it, f4& gx, f4& ux) const {
+    const float a = ldexpf(1.f, -ge[it]), b = ldexpf(1.f, -ue[it]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) gx[i] = (float)g[it][i] * a, ux[i] = (float)u[it][i] * b;
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ void ff_put(T* to, const f4& x) {
+  if constexpr (sizeof(T) == 2)
+    st4(reinterpret_cast<__bf16*>(to), x[0], x[1], x[2], x[3]);
+  else
+    *reinterpret_cast<f4*>(to) = x;
+}
+
+// act(g) and, where wanted, its slope
+template <bool SLOPE>
+__device__ __forceinline__ void ff_act(int act, float g, float& a, float& slope) {
+  slope = 0.f;
+  if (act == 0) {  // SiLU; the logistic function by 2^x and the reciprocal, an ulp each
+    const float s = __builtin_amdgcn_rcpf(1.f + ex2(g * -kLog2e));
+    a = g * s;
+    if constexpr (SLOPE) slope = s * (1.f + g * (1.f - s));
+  } else {  // GELU
+    const float s = 0.5f * (1.f + erff(g * 0.70710678118654752f));
+    a = g * s;
+    if constexpr (SLOPE) slope = s + g * expf(-0.5f * g * g) * 0.39894228040143268f;
   }
 }
 
@@ -179,15 +199,88 @@ __device__ __forceinline__ void ff_wave_order() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// a strip's products, in the lanes' layout, through the wave's place in LDS
-template <typename T, int FORM, int END, int BM, int BN>
-__device__ __forceinline__ void ff_leave(const FfArgs<T>& p, const f4* x, float* s, int64_t m, int64_t n, int lane) {
-  using Z = FfTile<T, FORM, END, BM, BN>;
+// A strip's products x, in the lanes' layout, through the wave's place in LDS (lds, BYTES of it).
+template <typename T, class S>
+__device__ __forceinline__ void ff_leave(const FfArgs<T>& p, const f4* x, float* lds, const S& s, const FfPast<T, S>* past,
+                                         int end, int lane) {
+  float* power = lds + 16 * S::SLD;  // of the row's blocks: g's, then u's
   ff_wave_order();
 #pragma unroll
-  for (int j = 0; j < Z::NT; ++j) *reinterpret_cast<f4*>(s + (lane & 15) * Z::SLD + 16 * j + 4 * (lane >> 4)) = x[j];
+  for (int j = 0; j < S::NT; ++j) *reinterpret_cast<f4*>(lds + (lane & 15) * S::SLD + 16 * j + 4 * (lane >> 4)) = x[j];
+  if constexpr (S::HALVES) {
+    if (p.hid.g) {
+      const int64_t nb = (p.N + kFfBlock - 1) / kFfBlock, row = s.m + (lane & 15);
+#pragma unroll
+      for (int b = 0; b < S::NB; ++b) {
+        float most = 0.f;
+#pragma unroll
+        for (int j = 2 * b; j < 2 * b + 2; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float v = fabsf(x[j][i]);
+            most = v <= 3.0e38f ? fmaxf(most, v) : most;
+          }
+        most = fmaxf(most, row_partner16(most, (lane & 16) != 0));
+        most = fmaxf(most, row_partner32(most, lane >= 32));
+        const int sh = state_shift(most);
+        const int64_t col = s.n + kFfBlock * (b % (S::NB / 2));
+        if (lane < 16) {
+          power[lane * S::NB + b] = ldexpf(1.f, sh);
+          if (row < p.M && col < p.N) (b < S::NB / 2 ? p.hid.ge : p.hid.ue)[row * nb + col / kFfBlock] = (int8_t)sh;
+        }
+      }
+    }
+  }
   ff_wave_order();
-  ff_strip<T, FORM, END, BM, BN>(p, s, m, n, lane);
+  const int rows = s.rows(p);
+  const int64_t row0 = s.m + s.r, col = s.n + s.c;
+  int64_t at = row0 * p.N + col;
+#pragma unroll
+  for (int it = 0; it < S::IT; ++it, at += S::RI * p.N) {
+    if (it >= rows) continue;
+    const int r = s.r + S::RI * it;
+    const f4 v = *reinterpret_cast<const f4*>(lds + r * S::SLD + s.c);
+    if (end == FF_STORE) {
+      ff_put((s.m + r < p.cut ? p.c[0] : p.c[1] - p.cut * p.N) + at, v);
+    } else if (end == FF_GATE) {
+      const f4 u = *reinterpret_cast<const f4*>(lds + r * S::SLD + S::COLS + s.c);
+      if (p.hid.g) {
+        if constexpr (S::HALVES) {
+          const float fg = power[r * S::NB + s.c / kFfBlock], fu = power[r * S::NB + S::NB / 2 + s.c / kFfBlock];
+          *reinterpret_cast<f16x4*>(static_cast<_Float16*>(p.hid.g) + at) =
+              f16x4{(_Float16)(v[0] * fg), (_Float16)(v[1] * fg), (_Float16)(v[2] * fg), (_Float16)(v[3] * fg)};
+          *reinterpret_cast<f16x4*>(static_cast<_Float16*>(p.hid.u) + at) =
+              f16x4{(_Float16)(u[0] * fu), (_Float16)(u[1] * fu), (_Float16)(u[2] * fu), (_Float16)(u[3] * fu)};
+        } else {
+          *reinterpret_cast<f4*>(static_cast<float*>(p.hid.g) + at) = v;
+          *reinterpret_cast<f4*>(static_cast<float*>(p.hid.u) + at) = u;
+        }
+      }
+      if (p.h) {
+        f4 h;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float a, slope;
+          ff_act<false>(p.act, v[i], a, slope);
+          h[i] = a * u[i];
+        }
+        ff_put(p.h + at, h);
+      }
+    } else {
+      f4 g, u, dg, du;
+      past->get(it, g, u);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float a, slope;
+        ff_act<true>(p.act, g[i], a, slope);
+        dg[i] = v[i] * u[i] * slope;
+        du[i] = v[i] * a;
+      }
+      T* to = p.dgu + 2 * at - col;
+      ff_put(to, dg);
+      ff_put(to + p.N, du);
+    }
+  }
 }
 
 // The tile of a workgroup: XCDs take blocks in turn, so that a run of neighbouring tiles, eight of M by
@@ -327,34 +420,49 @@ __global__ __launch_bounds__(64 * (BM / 64) * 2, 2) void ff_kernel(FfArgs<T> p) 
   }
   ff_landed();  // (nothing is under way; said where a path from a load to the barrier is looked for)
   __syncthreads();
-  float* stage = reinterpret_cast<float*>(smem) + wave * (16 * Z::SLD);
-  const int64_t n = n0 + (END == FF_GATE ? Z::WN / 2 : Z::WN) * wn;
+  using S = FfStrip<T, FORM, END, BM, BN>;
+  static_assert(Z::NW * S::BYTES <= 2 * Z::BUF, "strips in the tiles' place");
+  float* stage = reinterpret_cast<float*>(smem + wave * S::BYTES);
+  const int64_t n = n0 + S::COLS * wn;
+  const auto strip = [&](int i) { return S(m0 + 64 * wm + 16 * i, n, lane); };
+  if constexpr (END == FF_GRAD) {  // a strip's g and u on their way while the strip before it leaves
+    FfPast<T, S> past[2];
+    past[0].load(p, strip(0));
 #pragma unroll
-  for (int i = 0; i < MT; ++i) ff_leave<T, FORM, END, BM, BN>(p, acc[i], stage, m0 + 64 * wm + 16 * i, n, lane);
+    for (int i = 0; i < MT; ++i) {
+      if (i + 1 < MT) past[(i + 1) & 1].load(p, strip(i + 1));
+      ff_leave<T, S>(p, acc[i], stage, strip(i), &past[i & 1], END, lane);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < MT; ++i) ff_leave<T, S>(p, acc[i], stage, strip(i), nullptr, END, lane);
+  }
 }
 
 // The parts of the tiles that were cut, a strip a wave
 template <typename T, int FORM, int END, int BM, int BN>
 __global__ __launch_bounds__(256) void ff_join_kernel(FfArgs<T> p) {
   using Z = FfTile<T, FORM, END, BM, BN>;
+  using S = FfStrip<T, FORM, END, BM, BN>;
   constexpr int STRIPS = Z::NW * Z::MT;
-  __shared__ __align__(16) float stage[4][16 * Z::SLD];
+  __shared__ __align__(16) unsigned char stage[4][S::BYTES];
   const int lane = threadIdx.x & 63, w4 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int q = blockIdx.x * 4 + w4, tile = q / STRIPS, strip = q % STRIPS, wave = strip / Z::MT, i = strip % Z::MT;
+  const int id = blockIdx.x * 4 + w4, tile = id / STRIPS, strip = id % STRIPS, wave = strip / Z::MT, i = strip % Z::MT;
   int im, in;
   ff_place(p.full + tile, p.tm * p.tn, p.tm, p.tn, im, in);
   f4 x[Z::NT];
   const float* from = p.part + (int64_t)tile * p.split * (BM * BN) + wave * (64 * Z::WN) + i * Z::NT * 256 + 4 * lane;
 #pragma unroll
   for (int j = 0; j < Z::NT; ++j) x[j] = *reinterpret_cast<const f4*>(from + j * 256);
-  for (int s = 1; s < p.split; ++s) {
+  for (int q = 1; q < p.split; ++q) {
     from += BM * BN;
 #pragma unroll
     for (int j = 0; j < Z::NT; ++j) x[j] += *reinterpret_cast<const f4*>(from + j * 256);
   }
-  const int64_t m = (int64_t)im * BM + 64 * (wave / Z::NWN) + 16 * i;
-  const int64_t n = (int64_t)in * Z::BNC + (END == FF_GATE ? Z::WN / 2 : Z::WN) * (wave % Z::NWN);
-  ff_leave<T, FORM, END, BM, BN>(p, x, stage[w4], m, n, lane);
+  const S s((int64_t)im * BM + 64 * (wave / Z::NWN) + 16 * i, (int64_t)in * Z::BNC + S::COLS * (wave % Z::NWN), lane);
+  FfPast<T, S> past;
+  if constexpr (END == FF_GRAD) past.load(p, s);
+  ff_leave<T, S>(p, x, reinterpret_cast<float*>(stage[w4]), s, &past, END, lane);
 }
 
 namespace {

@@ -15,8 +15,18 @@ enum FfForm : int { FF_ROWS = 0, FF_MIXED = 1, FF_COLUMNS = 2 };
 // What becomes of C:
 //     FF_STORE  rounded and stored
 //     FF_GATE   B is a pair, C a pair g, u: h = act(g) u, and g, u themselves where asked for
-//     FF_GRAD   C is dh: h, dg and du from it and the stored g, u
+//     FF_GRAD   C is dh: dg and du from it and the stored g, u
 enum FfEnd : int { FF_STORE = 0, FF_GATE = 1, FF_GRAD = 2 };
+
+// g and u on their way from the forward to the backward, (M, N): fp32 problems as they are; bf16 ones in
+// fp16, with a power of two for every row and 32 channels that takes their largest finite magnitude to
+// [2^14, 2^15): 2^-12 of a value against the 2^-9 that the gradients are rounded by, at half the bytes.
+constexpr int kFfBlock = 32;
+template <typename T>
+struct FfHidden {
+  void *g, *u;       // float or _Float16
+  int8_t *ge, *ue;   // bf16 problems: the powers, (M, ceil(N / 32)): stored = value 2^power
+};
 
 template <typename T>
 struct FfArgs {
@@ -27,8 +37,8 @@ struct FfArgs {
   int pairs;
   T* c[2];            // FF_STORE: rows from `cut` on are those of c[1]
   int64_t cut;
-  float *g, *u;       // (M, N); FF_GATE: nullable; FF_GRAD: read
-  T *h, *dgu;         // h (M, N), nullable; dg, du side by side (M, 2 N)
+  FfHidden<T> hid;    // FF_GATE: written where hid.g is given; FF_GRAD: read
+  T *h, *dgu;         // FF_GATE: h (M, N), nullable; FF_GRAD: dg, du side by side (M, 2 N)
   int act;
   // set by the launch
   float* part;        // partial tiles

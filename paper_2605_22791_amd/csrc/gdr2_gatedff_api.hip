@@ -44,10 +44,10 @@ FfArgs<T> ff_args(int64_t M, int64_t N, int64_t K, const void* a, int64_t lda, c
   return p;
 }
 
-// fp32 g and u (rows, F), first: what a saving forward leaves; h (rows, F); backward also the
-// gradients at g and u (rows, 2 F); partial tiles of the products
+// h (rows, F), and for a backward g and u with it, first: what a saving forward leaves; the gradients
+// at g and u (rows, 2 F); partial tiles of the products
 struct FfLayout {
-  size_t g, u, h, dgu, part, total;
+  size_t h, g, u, ge, ue, dgu, part, total;
 };
 template <typename T>
 FfLayout ff_layout_of(const gdr2_gatedff* p, bool bwd) {
@@ -60,12 +60,15 @@ FfLayout ff_layout_of(const gdr2_gatedff* p, bool bwd) {
     off += round_up(bytes);
     return at;
   };
-  if (bwd) {
-    L.g = take(4 * n);
-    L.u = take(4 * n);
-  }
   L.h = take(e * n);
-  if (bwd) L.dgu = take(2 * e * n);
+  if (bwd) {
+    L.g = take(e * n);
+    L.u = take(e * n);
+    const size_t powers = e == 2 ? (size_t)M * ((F + kFfBlock - 1) / kFfBlock) : 0;
+    L.ge = take(powers);
+    L.ue = take(powers);
+    L.dgu = take(2 * e * n);
+  }
   size_t part = 0;
   const auto product = [&](int form, int end, int64_t M, int64_t N, int64_t K, int pairs) {
     part = std::max(part, ff_part_bytes<T>(form, end, M, N, K, pairs));
@@ -88,13 +91,17 @@ FfLayout ff_layout(const gdr2_gatedff* p, bool bwd) {
   return p->dtype == GDR2_FP32 ? ff_layout_of<float>(p, bwd) : ff_layout_of<bf16_t>(p, bwd);
 }
 
+template <typename T>
+FfHidden<T> ff_hidden(void* ws, const FfLayout& L) {
+  return {at<char>(ws, L.g), at<char>(ws, L.u), at<int8_t>(ws, L.ge), at<int8_t>(ws, L.ue)};
+}
+
 // h and, where they are asked for, g and u
 template <typename T>
-hipError_t ff_gate(const gdr2_gatedff* p, const void* x, const void* Wg, const void* Wu, float* g, float* u, T* h, void* part,
-                   hipStream_t st) {
+hipError_t ff_gate(const gdr2_gatedff* p, const void* x, const void* Wg, const void* Wu, T* h, const FfHidden<T>& hid,
+                   void* part, hipStream_t st) {
   FfArgs<T> a = ff_args<T>(p->rows, p->F, p->D, x, p->D, Wg, Wu, p->D, part);
-  a.g = g;
-  a.u = u;
+  a.hid = hid;
   a.h = h;
   a.act = p->act;
   return launch_ff<T, FF_ROWS, FF_GATE>(a, st);
@@ -125,7 +132,7 @@ gdr2_status gdr2_gatedff_fwd(const gdr2_gatedff* p, const void* x, const void* W
     using T = decltype(t);
     T* h = at<T>(ws, L.h);
     void* part = at<char>(ws, L.part);
-    hipError_t e = ff_gate<T>(p, x, Wg, Wu, save ? at<float>(ws, L.g) : nullptr, save ? at<float>(ws, L.u) : nullptr, h, part, stream);
+    hipError_t e = ff_gate<T>(p, x, Wg, Wu, h, save ? ff_hidden<T>(ws, L) : FfHidden<T>{}, part, stream);
     if (e != hipSuccess) return e;
     FfArgs<T> a = ff_args<T>(p->rows, p->D, p->F, h, p->F, Wd, nullptr, p->F, part);
     a.c[0] = static_cast<T*>(y);
@@ -149,18 +156,16 @@ gdr2_status gdr2_gatedff_bwd(const gdr2_gatedff* p, const void* x, const void* W
   if (ws_bytes < L.total) return GDR2_EWORKSPACE;
   const auto run = [&](auto t) {
     using T = decltype(t);
-    float *g = at<float>(ws, L.g), *u = at<float>(ws, L.u);
+    const FfHidden<T> hid = ff_hidden<T>(ws, L);
     T *h = at<T>(ws, L.h), *dgu = at<T>(ws, L.dgu);
     void* part = at<char>(ws, L.part);
     const int64_t M = p->rows, D = p->D, F = p->F;
     hipError_t e = hipSuccess;
     if (M > 0) {
-      if (!saved) e = ff_gate<T>(p, x, Wg, Wu, g, u, nullptr, part, stream);
+      if (!saved) e = ff_gate<T>(p, x, Wg, Wu, weights ? h : nullptr, hid, part, stream);
       if (e != hipSuccess) return e;
       FfArgs<T> a = ff_args<T>(M, F, D, dy, D, Wd, nullptr, F, part);
-      a.g = g;
-      a.u = u;
-      a.h = weights ? h : nullptr;
+      a.hid = hid;
       a.dgu = dgu;
       a.act = p->act;
       e = launch_ff<T, FF_MIXED, FF_GRAD>(a, stream);
