@@ -465,6 +465,103 @@ __global__ __launch_bounds__(256) void ff_join_kernel(FfArgs<T> p) {
   ff_leave<T, S>(p, x, reinterpret_cast<float*>(stage[w4]), s, &past, END, lane);
 }
 
+// Few rows of A (up to 16 MT): the weights' way through memory is all there is.  A workgroup takes 16 rows of
+// B (FF_GATE: of each of the pair), its eight waves a part of the sum each, AHEAD steps of 64 bytes a row
+// on their way at a time.  Loads have four lanes a row (16 address cycles; a row a lane, as the fragments
+// have it, takes 64, and was 13.4 us where this is THIN_US) and pass through the wave's own place in
+// LDS; the waves' sums meet there too, in order.
+template <typename T, int END, int MT>
+__global__ __launch_bounds__(512) void ff_thin_kernel(FfArgs<T> p) {
+  using F = FfType<T>;
+  using Frag = typename F::Frag;
+  constexpr int P = END == FF_GATE ? 2 : 1, KF = 16 / (int)sizeof(T), KS = 4 * KF;  // elements of a piece, of a step
+  // FF_GATE: two workgroups a CU; else it has a workgroup a CU or less
+  constexpr int AHEAD = P == 2 ? (MT == 1 ? 3 : MT == 2 ? 2 : 1) : (MT == 1 ? 8 : MT == 2 ? 5 : 3);
+  constexpr int NW = 8, OWN = AHEAD * (P + MT) * 1024, ALL = NW * (OWN > P * MT * 1024 ? OWN : P * MT * 1024);
+  __shared__ __align__(16) unsigned char smem[ALL];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane >> 2, lq = lane & 3;  // the row and the piece that the lane loads
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  const int steps = (int)((p.K + KS - 1) / KS), s0 = (int)((int64_t)steps * wave / NW), s1 = (int)((int64_t)steps * (wave + 1) / NW);
+  const T *b[P], *a[MT];
+#pragma unroll
+  for (int q = 0; q < P; ++q) b[q] = p.b[q] + min(n0 + lr, p.N - 1) * p.ldb + KF * lq;
+#pragma unroll
+  for (int i = 0; i < MT; ++i) a[i] = p.a + min((int64_t)(16 * i + lr), p.M - 1) * p.lda + KF * lq;
+  f4 acc[P][MT];
+#pragma unroll
+  for (int q = 0; q < P; ++q)
+#pragma unroll
+    for (int i = 0; i < MT; ++i) acc[q][i] = f4zero();
+  const u4v zero = {0, 0, 0, 0};
+  const auto piece = [&](const T* x, int s) {  // what lies past the sum's end is zero
+    const int64_t k = (int64_t)s * KS;
+    return s < s1 && k + KF * lq < p.K ? ldg16(x + k) : zero;
+  };
+  // 16 rows of 64 bytes, pieces exchanged between rows below and from 8: 16 lanes are read at a time, of
+  // rows {0-3, 8-11} or {4-7, 12-15} and two neighbouring pieces
+  unsigned char* own = smem + wave * OWN;
+  const int put = 64 * lr + ((lq ^ (lr >> 3 << 1)) << 4);
+  const int get = 64 * (lane & 15) + (((lane >> 4) ^ ((lane >> 3 & 1) << 1)) << 4);
+  for (int s = s0; s < s1; s += AHEAD) {
+    u4v w[AHEAD][P], x[AHEAD][MT];
+#pragma unroll
+    for (int v = 0; v < AHEAD; ++v) {
+#pragma unroll
+      for (int q = 0; q < P; ++q) w[v][q] = piece(b[q], s + v);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) x[v][i] = piece(a[i], s + v);
+    }
+    ff_wave_order();
+#pragma unroll
+    for (int v = 0; v < AHEAD; ++v) {
+#pragma unroll
+      for (int q = 0; q < P; ++q) sts16(own + (v * (P + MT) + q) * 1024 + put, w[v][q]);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) sts16(own + (v * (P + MT) + P + i) * 1024 + put, x[v][i]);
+    }
+    ff_wave_order();
+#pragma unroll
+    for (int v = 0; v < AHEAD; ++v) {
+      const auto frag = [&](int k) { return *reinterpret_cast<const Frag*>(own + (v * (P + MT) + k) * 1024 + get); };
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const Frag f = frag(P + i);
+#pragma unroll
+        for (int q = 0; q < P; ++q) acc[q][i] = F::mma(frag(q), f, acc[q][i]);
+      }
+    }
+  }
+  __syncthreads();
+  float(*sum)[P * MT][256] = reinterpret_cast<float(*)[P * MT][256]>(smem);
+#pragma unroll
+  for (int q = 0; q < P; ++q)
+#pragma unroll
+    for (int i = 0; i < MT; ++i) *reinterpret_cast<f4*>(&sum[wave][q * MT + i][4 * lane]) = acc[q][i];
+  __syncthreads();
+  // neighbouring threads, neighbouring columns of C
+  for (int e = tid; e < 256 * MT; e += 64 * NW) {
+    const int c = e & 15, m = e >> 4, at = 4 * (16 * (c >> 2) + (m & 15)) + (c & 3);
+    if (m >= p.M || n0 + c >= p.N) continue;
+    float v[P];
+#pragma unroll
+    for (int q = 0; q < P; ++q) {
+      v[q] = sum[0][q * MT + (m >> 4)][at];
+      for (int w = 1; w < NW; ++w) v[q] += sum[w][q * MT + (m >> 4)][at];
+    }
+    T* to = (END == FF_GATE ? p.h : p.c[0]) + (int64_t)m * p.N + n0 + c;
+    if constexpr (END == FF_GATE) {
+      float act, slope;
+      ff_act<false>(p.act, v[0], act, slope);
+      v[0] = act * v[1];
+    }
+    if constexpr (sizeof(T) == 2)
+      *reinterpret_cast<__bf16*>(to) = (__bf16)v[0];
+    else
+      *to = v[0];
+  }
+}
+
 namespace {
 
 struct FfPlan {
@@ -507,6 +604,14 @@ hipError_t ff_go(const FfArgs<T>& a, hipStream_t st) {
 
 }  // namespace
 
+namespace {
+template <typename T, int END, int MT>
+hipError_t ff_thin(const FfArgs<T>& a, hipStream_t st) {
+  hipLaunchKernelGGL((ff_thin_kernel<T, END, MT>), dim3((unsigned)((a.N + 15) / 16)), dim3(512), 0, st, a);
+  return hipGetLastError();
+}
+}  // namespace
+
 template <typename T>
 size_t ff_part_bytes(int form, int end, int64_t M, int64_t N, int64_t K, int pairs) {
   const FfPlan q = ff_choose(end, M, N, K, pairs, sizeof(T));
@@ -515,6 +620,12 @@ size_t ff_part_bytes(int form, int end, int64_t M, int64_t N, int64_t K, int pai
 
 template <typename T, int FORM, int END>
 hipError_t launch_ff(FfArgs<T> a, hipStream_t st) {
+  if constexpr (FORM == FF_ROWS && END != FF_GRAD)
+    if (a.M <= 64 && !a.hid.g) {  // (a saving forward gives the bits of the backward's own g and u)
+      if (a.M <= 16) return ff_thin<T, END, 1>(a, st);
+      if (a.M <= 32) return ff_thin<T, END, 2>(a, st);
+      return ff_thin<T, END, 4>(a, st);
+    }
   const FfPlan q = ff_choose(END, a.M, a.N, a.K, a.pairs, sizeof(T));
   a.tm = q.tm;
   a.tn = q.tn;
