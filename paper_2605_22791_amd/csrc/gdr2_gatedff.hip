@@ -53,9 +53,10 @@ struct FfType<float> {
 __device__ __forceinline__ int ff_row_swz(int r) { return (r & 2) | ((r & 8) >> 1); }
 // Columns: STEP / E rows of ROWS elements.  bf16: the transposing load serves 32 lanes at a time, 32 bytes
 // of rows {0-3, 8-11} (+ 4); fp32: four rows, four apart, of 64 bytes.
-template <typename T>
+template <typename T, int RB>  // bytes of a row
 __device__ __forceinline__ int ff_col_swz(int k) {
-  return sizeof(T) == 2 ? ((k & 3) | ((k & 8) >> 1)) << 1 : (k >> 2 & 3) << 2;
+  if (sizeof(T) == 4) return (k >> 2 & 3) << 2;
+  return RB == 128 ? ((k & 2) | (k & 8) >> 1) : ((k & 3) | ((k & 8) >> 1)) << 1;
 }
 
 // One operand's way into LDS: ROWS x 128 bytes by NW waves, 1 KB an instruction.
@@ -71,7 +72,7 @@ struct FfLoad {
   int piece;     // and the lane's piece there
   __device__ __forceinline__ FfLoad(unsigned ld, int lane, int wave) {  // ld: bytes from row to row
     const int r = wave * RI + lane / (RB / 16);
-    piece = (lane % (RB / 16)) ^ (COL ? ff_col_swz<T>(r) : ff_row_swz(r));
+    piece = (lane % (RB / 16)) ^ (COL ? ff_col_swz<T, RB>(r) : ff_row_swz(r));
     row = r * ld;
   }
   __device__ __forceinline__ unsigned at(int i, unsigned ld) const {
@@ -96,11 +97,14 @@ constexpr unsigned kOutside = 0x80000000u;  // an offset past every buffer
 
 }  // namespace
 
+constexpr int ff_waves_m(int bm) { return bm == 64 ? 2 : bm / 64; }  // waves along M, two along N
+constexpr int ff_threads(int bm) { return 128 * ff_waves_m(bm); }
+
 template <typename T, int FORM, int END, int BM, int BN>
 struct FfTile {
   static constexpr int E = sizeof(T);
-  static constexpr int NWM = BM / 64, NWN = 2, NW = NWM * NWN;  // waves of 64 x BN / 2
-  static constexpr int WN = BN / NWN, MT = 4, NT = WN / 16;
+  static constexpr int NWM = ff_waves_m(BM), NWN = 2, NW = NWM * NWN, WM = BM / NWM;  // waves of WM x WN
+  static constexpr int WN = BN / NWN, MT = WM / 16, NT = WN / 16;
   static constexpr int BK = STEP / E;
   static constexpr bool ACOL = FORM == FF_COLUMNS, BCOL = FORM != FF_ROWS;
   static constexpr int BUF = (BM + BN) * STEP;
@@ -116,6 +120,7 @@ struct FfStrip : FfTile<T, FORM, END, BM, BN> {
   static constexpr int COLS = END == FF_GATE ? Z::WN / 2 : Z::WN, LR = COLS / 4, RI = 64 / LR, IT = 16 / RI;
   static constexpr bool HALVES = END == FF_GATE && sizeof(T) == 2;
   static constexpr int NB = Z::WN / kFfBlock;                  // blocks of a row of the strip with a power of their own
+  static_assert(!HALVES || COLS % kFfBlock == 0, "whole blocks");
   static constexpr int BYTES = 16 * (Z::SLD + (HALVES ? NB : 0)) * 4;  // LDS of a wave
   int64_t m, n;  // the strip's first row and column
   int r, c;      // the lane's first row and its columns, within the strip
@@ -285,17 +290,24 @@ __device__ __forceinline__ void ff_leave(const FfArgs<T>& p, const f4* x, float*
 
 // The tile of a workgroup: XCDs take blocks in turn, so that a run of neighbouring tiles, eight of M by
 // as many of N, is on one and shares its L2.
-__device__ __forceinline__ void ff_place(int t, int tiles, int tm, int tn, int& im, int& in) {
-  const int per = tiles / 8, rest = tiles % 8, x = t % 8;
+// FF_COLUMNS: from tile tm tn on those of the second product, which p then becomes.
+template <typename T, int FORM>
+__device__ __forceinline__ void ff_place(FfArgs<T>& p, int t, int& im, int& in) {
+  const int per = p.tiles / 8, rest = p.tiles % 8, x = t % 8;
   t = x * per + min(x, rest) + t / 8;
+  if constexpr (FORM == FF_COLUMNS)
+    if (t >= p.tm * p.tn) {
+      t -= p.tm * p.tn;
+      static_cast<FfProduct<T>&>(p) = p.also;
+    }
   constexpr int GM = 8;
-  const int group = t / (GM * tn), first = group * GM, rows = min(GM, tm - first), k = t - group * GM * tn;
+  const int group = t / (GM * p.tn), first = group * GM, rows = min(GM, p.tm - first), k = t - group * GM * p.tn;
   im = first + k % rows;
   in = k / rows;
 }
 
 template <typename T, int FORM, int END, int BM, int BN>
-__global__ __launch_bounds__(64 * (BM / 64) * 2, 2) void ff_kernel(FfArgs<T> p) {
+__global__ __launch_bounds__(ff_threads(BM), 2) void ff_kernel(FfArgs<T> p) {
   using Z = FfTile<T, FORM, END, BM, BN>;
   using F = FfType<T>;
   using Frag = typename F::Frag;
@@ -303,16 +315,16 @@ __global__ __launch_bounds__(64 * (BM / 64) * 2, 2) void ff_kernel(FfArgs<T> p) 
   __shared__ __align__(1024) unsigned char smem[2 * Z::BUF];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / Z::NWN, wn = wave % Z::NWN, r16 = lane & 15, grp = lane >> 4;
-  const int tiles = p.tm * p.tn;
   // whole tiles first; then parts of the others, a tile's parts apart
   int t = blockIdx.x, part = 0, im, in;
   if (t >= p.full) {
-    const int left = tiles - p.full;
+    const int left = p.tiles - p.full;
     part = (t - p.full) / left;
     t = p.full + (t - p.full) % left;
   }
   const bool whole = t < p.full;
-  ff_place(t, tiles, p.tm, p.tn, im, in);
+  const int cut = t - p.full;  // its number among those that are cut
+  ff_place<T, FORM>(p, t, im, in);
   const int64_t m0 = (int64_t)im * BM, n0 = (int64_t)in * Z::BNC;
   const int per = (int)((p.K + Z::BK - 1) / Z::BK), steps = per * p.pairs;  // steps of one product, of all
   const int s0 = whole ? 0 : (int)((int64_t)steps * part / p.split);
@@ -368,17 +380,18 @@ __global__ __launch_bounds__(64 * (BM / 64) * 2, 2) void ff_kernel(FfArgs<T> p) 
   const auto rows_frag = [&](const unsigned char* s, int r0, int ks) {
     return *reinterpret_cast<const Frag*>(s + (r0 + r16) * STEP + (((4 * ks + grp) ^ ff_row_swz(r16)) << 4));
   };
-  const auto cols_frag = [&](const unsigned char* s, int rb, int r0, int ks) {
+  const auto cols_frag = [&](const unsigned char* s, auto row_bytes, int r0, int ks) {
+    constexpr int RB = decltype(row_bytes)::value;
     Frag x;
     if constexpr (E == 2) {
       const int k = 32 * ks + 8 * grp + (r16 >> 2);
-      const unsigned char* q = s + k * rb + (((2 * (r0 / 16)) ^ ff_col_swz<T>(k)) << 4) + 8 * (r16 & 3);
-      x = ld_tr8p(reinterpret_cast<const __bf16*>(q), reinterpret_cast<const __bf16*>(q + 4 * rb));
+      const unsigned char* q = s + k * RB + (((2 * (r0 / 16)) ^ ff_col_swz<T, RB>(k)) << 4) + 8 * (r16 & 3);
+      x = ld_tr8p(reinterpret_cast<const __bf16*>(q), reinterpret_cast<const __bf16*>(q + 4 * RB));
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int k = 16 * ks + 4 * grp + i;
-        x[i] = *reinterpret_cast<const float*>(s + k * rb + (((r0 / 4) ^ ff_col_swz<T>(k)) << 4) + 4 * r16);
+        x[i] = *reinterpret_cast<const float*>(s + k * RB + (((r0 / 4) ^ ff_col_swz<T, RB>(k)) << 4) + 4 * r16);
       }
     }
     return x;
@@ -399,10 +412,10 @@ __global__ __launch_bounds__(64 * (BM / 64) * 2, 2) void ff_kernel(FfArgs<T> p) 
       Frag a[MT], b[NT];
 #pragma unroll
       for (int i = 0; i < MT; ++i)
-        a[i] = Z::ACOL ? cols_frag(sa, BM * E, 64 * wm + 16 * i, ks) : rows_frag(sa, 64 * wm + 16 * i, ks);
+        a[i] = Z::ACOL ? cols_frag(sa, std::integral_constant<int, BM * E>{}, Z::WM * wm + 16 * i, ks) : rows_frag(sa, Z::WM * wm + 16 * i, ks);
 #pragma unroll
       for (int j = 0; j < NT; ++j)
-        b[j] = Z::BCOL ? cols_frag(sb, BN * E, Z::WN * wn + 16 * j, ks) : rows_frag(sb, Z::WN * wn + 16 * j, ks);
+        b[j] = Z::BCOL ? cols_frag(sb, std::integral_constant<int, BN * E>{}, Z::WN * wn + 16 * j, ks) : rows_frag(sb, Z::WN * wn + 16 * j, ks);
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -410,8 +423,8 @@ __global__ __launch_bounds__(64 * (BM / 64) * 2, 2) void ff_kernel(FfArgs<T> p) 
     }
   }
   if (!whole) {  // the lanes' registers as they are: 16 bytes a lane and instruction
-    const int64_t slot = (int64_t)(t - p.full) * p.split + part;
-    float* to = p.part + slot * (BM * BN) + wave * (64 * Z::WN) + 4 * lane;
+    const int64_t slot = (int64_t)cut * p.split + part;
+    float* to = p.part + slot * (BM * BN) + wave * (Z::WM * Z::WN) + 4 * lane;
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -424,7 +437,7 @@ __global__ __launch_bounds__(64 * (BM / 64) * 2, 2) void ff_kernel(FfArgs<T> p) 
   static_assert(Z::NW * S::BYTES <= 2 * Z::BUF, "strips in the tiles' place");
   float* stage = reinterpret_cast<float*>(smem + wave * S::BYTES);
   const int64_t n = n0 + S::COLS * wn;
-  const auto strip = [&](int i) { return S(m0 + 64 * wm + 16 * i, n, lane); };
+  const auto strip = [&](int i) { return S(m0 + Z::WM * wm + 16 * i, n, lane); };
   if constexpr (END == FF_GRAD) {  // a strip's g and u on their way while the strip before it leaves
     FfPast<T, S> past[2];
     past[0].load(p, strip(0));
@@ -449,9 +462,9 @@ __global__ __launch_bounds__(256) void ff_join_kernel(FfArgs<T> p) {
   const int lane = threadIdx.x & 63, w4 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int id = blockIdx.x * 4 + w4, tile = id / STRIPS, strip = id % STRIPS, wave = strip / Z::MT, i = strip % Z::MT;
   int im, in;
-  ff_place(p.full + tile, p.tm * p.tn, p.tm, p.tn, im, in);
+  ff_place<T, FORM>(p, p.full + tile, im, in);
   f4 x[Z::NT];
-  const float* from = p.part + (int64_t)tile * p.split * (BM * BN) + wave * (64 * Z::WN) + i * Z::NT * 256 + 4 * lane;
+  const float* from = p.part + (int64_t)tile * p.split * (BM * BN) + wave * (Z::WM * Z::WN) + i * Z::NT * 256 + 4 * lane;
 #pragma unroll
   for (int j = 0; j < Z::NT; ++j) x[j] = *reinterpret_cast<const f4*>(from + j * 256);
   for (int q = 1; q < p.split; ++q) {
@@ -459,7 +472,7 @@ __global__ __launch_bounds__(256) void ff_join_kernel(FfArgs<T> p) {
 #pragma unroll
     for (int j = 0; j < Z::NT; ++j) x[j] += *reinterpret_cast<const f4*>(from + j * 256);
   }
-  const S s((int64_t)im * BM + 64 * (wave / Z::NWN) + 16 * i, (int64_t)in * Z::BNC + S::COLS * (wave % Z::NWN), lane);
+  const S s((int64_t)im * BM + Z::WM * (wave / Z::NWN) + 16 * i, (int64_t)in * Z::BNC + S::COLS * (wave % Z::NWN), lane);
   FfPast<T, S> past;
   if constexpr (END == FF_GRAD) past.load(p, s);
   ff_leave<T, S>(p, x, reinterpret_cast<float*>(stage[w4]), s, &past, END, lane);
@@ -468,7 +481,8 @@ __global__ __launch_bounds__(256) void ff_join_kernel(FfArgs<T> p) {
 // Few rows of A (up to 16 MT): the weights' way through memory is all there is.  A workgroup takes 16 rows of
 // B (FF_GATE: of each of the pair), its eight waves a part of the sum each, AHEAD steps of 64 bytes a row
 // on their way at a time.  Loads have four lanes a row (16 address cycles; a row a lane, as the fragments
-// have it, takes 64, and was 13.4 us where this is THIN_US) and pass through the wave's own place in
+// have it, takes 64, and took 13.4 us where this takes 11.4:
+// one token, F = 5504 pairs of 2048, 4.0 TB/s) and pass through the wave's own place in
 // LDS; the waves' sums meet there too, in order.
 template <typename T, int END, int MT>
 __global__ __launch_bounds__(512) void ff_thin_kernel(FfArgs<T> p) {
@@ -564,39 +578,72 @@ __global__ __launch_bounds__(512) void ff_thin_kernel(FfArgs<T> p) {
 
 namespace {
 
+// How a call is laid out: the tile size and what the tiles left over are cut into, by the time that they
+// would take, in us: rounds of as many tiles as there are places, a part of a round for those that are
+// cut, and parts' way through memory and a launch.  Rates measured: 256 x 256 tiles 1.2 PFLOP/s in bf16, 128 x 128
+// 1.0, 64 x 64 (four a CU; FF_GATE: 64 x 128) 0.6; in fp32 0.1 either way.  Against each size by itself, 18 bf16
+// and 7 fp32 problems of 64 to 16000 rows, the choice was the best or within 9 % of it, both ways.
 struct FfPlan {
-  int bm, bn, tm, tn, full, split, slots;
+  int bm, bn, slots;
+  int tm[2], tn[2], tiles, full, split;
+  double us;
 };
-FfPlan ff_plan(int end, int64_t M, int64_t N, int64_t K, int pairs, int E, bool large) {
+// sizes of one or two products with the same sum
+struct FfSize {
+  int64_t M[2], N[2], K;
+  int pairs;
+};
+FfPlan ff_plan(int end, const FfSize& z, int E, int bm, int bn, int a_cu, double rate) {
   FfPlan q{};
-  q.bm = q.bn = large ? 256 : 128;
-  q.slots = large ? kCUs : 2 * kCUs;
-  const int bnc = end == FF_GATE ? q.bn / 2 : q.bn;
-  q.tm = (int)((M + q.bm - 1) / q.bm);
-  q.tn = (int)((N + bnc - 1) / bnc);
-  const int64_t tiles = (int64_t)q.tm * q.tn, steps = (K + STEP / E - 1) / (STEP / E) * pairs;
-  q.full = (int)(tiles / q.slots * q.slots);
-  const int64_t left = tiles - q.full;
+  q.bm = bm;
+  q.bn = bn;
+  q.slots = a_cu * kCUs;
+  int64_t tiles = 0;
+  for (int k = 0; k < 2; ++k) {
+    const int bnc = end == FF_GATE ? bn / 2 : bn;
+    q.tm[k] = (int)((z.M[k] + bm - 1) / bm);
+    q.tn[k] = (int)((z.N[k] + bnc - 1) / bnc);
+    tiles += (int64_t)q.tm[k] * q.tn[k];
+  }
+  q.tiles = (int)tiles;
+  const int64_t steps = (z.K + STEP / E - 1) / (STEP / E) * z.pairs, left = tiles % q.slots;
+  const double tile = 2e-9 * bm * bn * (double)(steps * (STEP / E)) / (rate / q.slots);  // us; rate in PFLOP/s
+  q.full = q.tiles;
   q.split = 1;
-  if (left > 0) q.split = (int)std::max<int64_t>(1, std::min<int64_t>(q.slots / left, steps / 4));
-  if (q.split == 1) q.full = (int)tiles;
+  q.us = tile * (double)((tiles + q.slots - 1) / q.slots);
+  for (int64_t split = 2; left > 0 && split <= q.slots / left && split <= steps / 4; ++split) {
+    const double us = tile * ((double)(tiles / q.slots) + 1.0 / split) + 4.0 + (double)left * split * bm * bn * 8.0 / 4.8e6;
+    if (us < q.us) {
+      q.us = us;
+      q.split = (int)split;
+      q.full = (int)(tiles - left);
+    }
+  }
   return q;
 }
-// 256 x 256 tiles where they give every CU one
-FfPlan ff_choose(int end, int64_t M, int64_t N, int64_t K, int pairs, int E) {
-  const FfPlan large = ff_plan(end, M, N, K, pairs, E, true);
-  if (E == 2 && (int64_t)large.tm * large.tn >= kCUs) return large;
-  return ff_plan(end, M, N, K, pairs, E, false);
+FfPlan ff_choose(int end, const FfSize& z, int E) {
+  const FfPlan mid = ff_plan(end, z, E, 128, 128, 2, E == 2 ? 1.0 : 0.1);
+  const FfPlan small = ff_plan(end, z, E, 64, E == 2 && end == FF_GATE ? 128 : 64, 4, E == 2 ? 0.6 : 0.1);
+  const FfPlan& best = small.us < mid.us ? small : mid;
+  if (E == 4) return best;
+  const FfPlan large = ff_plan(end, z, E, 256, 256, 1, 1.2);
+  return best.us < large.us ? best : large;
+}
+size_t ff_part_bytes(const FfPlan& q) { return (size_t)(q.tiles - q.full) * q.split * q.bm * q.bn * 4; }
+
+template <typename T>
+FfSize ff_size(const FfArgs<T>& a) {
+  return {{a.M, a.also.M}, {a.N, a.also.N}, a.K, a.pairs};
 }
 
-template <typename T, int FORM, int END, int BM>
+template <typename T, int FORM, int END, int BM, int BN>
 hipError_t ff_go(const FfArgs<T>& a, hipStream_t st) {
-  const int left = a.tm * a.tn - a.full;
-  hipLaunchKernelGGL((ff_kernel<T, FORM, END, BM, BM>), dim3((unsigned)(a.full + left * a.split)), dim3(64 * (BM / 64) * 2), 0, st, a);
+  using Z = FfTile<T, FORM, END, BM, BN>;
+  const int left = a.tiles - a.full;
+  hipLaunchKernelGGL((ff_kernel<T, FORM, END, BM, BN>), dim3((unsigned)(a.full + left * a.split)), dim3(ff_threads(BM)), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && left > 0) {
-    using Z = FfTile<T, FORM, END, BM, BM>;
-    hipLaunchKernelGGL((ff_join_kernel<T, FORM, END, BM, BM>), dim3((unsigned)(left * (Z::NW * Z::MT / 4))), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((ff_join_kernel<T, FORM, END, BM, BN>), dim3((unsigned)(left * (Z::NW * Z::MT / 4))), dim3(256), 0, st, a);
     e = hipGetLastError();
   }
   return e;
@@ -612,10 +659,9 @@ hipError_t ff_thin(const FfArgs<T>& a, hipStream_t st) {
 }
 }  // namespace
 
-template <typename T>
-size_t ff_part_bytes(int form, int end, int64_t M, int64_t N, int64_t K, int pairs) {
-  const FfPlan q = ff_choose(end, M, N, K, pairs, sizeof(T));
-  return (size_t)((int64_t)q.tm * q.tn - q.full) * q.split * q.bm * q.bn * 4;
+template <typename T, int FORM, int END>
+size_t ff_part_bytes(const FfArgs<T>& a) {
+  return ff_part_bytes(ff_choose(END, ff_size(a), sizeof(T)));
 }
 
 template <typename T, int FORM, int END>
@@ -626,23 +672,29 @@ hipError_t launch_ff(FfArgs<T> a, hipStream_t st) {
       if (a.M <= 32) return ff_thin<T, END, 2>(a, st);
       return ff_thin<T, END, 4>(a, st);
     }
-  const FfPlan q = ff_choose(END, a.M, a.N, a.K, a.pairs, sizeof(T));
-  a.tm = q.tm;
-  a.tn = q.tn;
+  const FfPlan q = ff_choose(END, ff_size(a), sizeof(T));
+  a.tm = q.tm[0];
+  a.tn = q.tn[0];
+  a.also.tm = q.tm[1];
+  a.also.tn = q.tn[1];
+  a.tiles = q.tiles;
   a.full = q.full;
   a.split = q.split;
   if constexpr (sizeof(T) == 2)
-    if (q.bm == 256) return ff_go<T, FORM, END, 256>(a, st);
-  return ff_go<T, FORM, END, 128>(a, st);
+    if (q.bm == 256) return ff_go<T, FORM, END, 256, 256>(a, st);
+  if (q.bm == 128) return ff_go<T, FORM, END, 128, 128>(a, st);
+  return ff_go<T, FORM, END, 64, sizeof(T) == 2 && END == FF_GATE ? 128 : 64>(a, st);
 }
 
-#define GDR2_FF(T)                                                        \
-  template size_t ff_part_bytes<T>(int, int, int64_t, int64_t, int64_t, int);   \
-  template hipError_t launch_ff<T, FF_ROWS, FF_STORE>(FfArgs<T>, hipStream_t);    \
-  template hipError_t launch_ff<T, FF_ROWS, FF_GATE>(FfArgs<T>, hipStream_t);     \
-  template hipError_t launch_ff<T, FF_MIXED, FF_STORE>(FfArgs<T>, hipStream_t);   \
-  template hipError_t launch_ff<T, FF_MIXED, FF_GRAD>(FfArgs<T>, hipStream_t);    \
-  template hipError_t launch_ff<T, FF_COLUMNS, FF_STORE>(FfArgs<T>, hipStream_t);
+#define GDR2_FF_ONE(T, FORM, END)                               \
+  template size_t ff_part_bytes<T, FORM, END>(const FfArgs<T>&); \
+  template hipError_t launch_ff<T, FORM, END>(FfArgs<T>, hipStream_t);
+#define GDR2_FF(T)                  \
+  GDR2_FF_ONE(T, FF_ROWS, FF_STORE)  \
+  GDR2_FF_ONE(T, FF_ROWS, FF_GATE)   \
+  GDR2_FF_ONE(T, FF_MIXED, FF_STORE) \
+  GDR2_FF_ONE(T, FF_MIXED, FF_GRAD)  \
+  GDR2_FF_ONE(T, FF_COLUMNS, FF_STORE)
 GDR2_FF(float)
 GDR2_FF(bf16_t)
 

@@ -29,26 +29,32 @@ struct FfHidden {
 };
 
 template <typename T>
-struct FfArgs {
+struct FfProduct {
   const T *a, *b[2];
   int64_t lda, ldb;   // elements from one row of memory to the next
-  int64_t M, N, K;
-  int64_t a2;         // pairs == 2: the second product's A starts a2 elements further; its B is b[1]
-  int pairs;
+  int64_t M, N;
   T* c[2];            // FF_STORE: rows from `cut` on are those of c[1]
   int64_t cut;
+  int tm, tn;         // tiles (set by the launch)
+};
+
+template <typename T>
+struct FfArgs : FfProduct<T> {
+  FfProduct<T> also;  // FF_COLUMNS: another product with the same sum, in the same launch (M = 0: none)
+  int64_t K;
+  int64_t a2;         // pairs == 2: the second product's A starts a2 elements further; its B is b[1]
+  int pairs;
   FfHidden<T> hid;    // FF_GATE: written where hid.g is given; FF_GRAD: read
   T *h, *dgu;         // FF_GATE: h (M, N), nullable; FF_GRAD: dg, du side by side (M, 2 N)
   int act;
-  // set by the launch
   float* part;        // partial tiles
-  int tm, tn;         // tiles
-  int full, split;    // tiles computed whole; parts of every other one
+  // set by the launch
+  int tiles, full, split;  // of them computed whole; parts of every other one
 };
 
-// Bytes of partial tiles that a call with these arguments takes.
-template <typename T>
-size_t ff_part_bytes(int form, int end, int64_t M, int64_t N, int64_t K, int pairs);
+// Bytes of partial tiles that a launch takes.
+template <typename T, int FORM, int END>
+size_t ff_part_bytes(const FfArgs<T>& a);
 template <typename T, int FORM, int END>
 hipError_t launch_ff(FfArgs<T> a, hipStream_t st);
 
