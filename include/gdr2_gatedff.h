@@ -11,8 +11,9 @@
  *     x, y, dy, dx      (rows, D)
  *     Wg, Wu, dWg, dWu  (F, D)
  *     Wd, dWd           (D, F)
- * D and F are multiples of 8 up to 65536, else GDR2_EUNSUPPORTED; rows from 0 to 2^24 (0 is
- * GDR2_OK: the forward does nothing, the backward sets the gradients of the weights to zero).
+ * D and F are multiples of 8 up to 65536, rows up to 2^24 and rows D and rows F below 2^36, else
+ * GDR2_EUNSUPPORTED.  rows = 0 is GDR2_OK: the forward does nothing, the backward sets the gradients
+ * of the weights to zero.
  * Products accumulate in fp32.  bf16 problems round h, and backward the gradients at g and u, to
  * bf16 once on their way into the products that read them; the backward reads g and u in 11 bits of
  * their own (a power of two for each row and 32 channels beside them), whether saved or formed again.

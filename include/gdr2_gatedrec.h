@@ -15,8 +15,9 @@
  *     x, i, o, dout, dx, di   (B, T, D)   problem->dtype (bf16 or fp32)
  *     g, dg                   (B, T, D)   fp32
  *     h0, h_T, h, dh_T, dh0   (B, D), packed (n_seqs, D)   fp32
- * Any D from 1 to 65536; up to 2^31 - 1 tokens (B T).  States are fp32 throughout; o and the
- * gradients are rounded once.
+ * Any D from 1 to 65536; up to 2^31 - 1 tokens (B T), and up to 2^23 workgroups, which take 64 tokens
+ * of 128 channels each (64 where D is odd or at most 64), else GDR2_EUNSUPPORTED.  States are fp32
+ * throughout; o and the gradients are rounded once.
  *
  * Packed batches (B = 1, n_seqs > 0): cu_seqlens (n_seqs + 1) holds the sequences' offsets,
  * 0 <= cu_seqlens[0] <= ... <= cu_seqlens[n_seqs] <= T; n_seqs = 0: fixed length, cu_seqlens

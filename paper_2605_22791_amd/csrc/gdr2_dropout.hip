@@ -53,11 +53,9 @@ __device__ __forceinline__ void drop_store(bf16_t* p, const float (&x)[EPL]) { s
 __device__ __forceinline__ void drop_store1(float* p, float x) { *p = x; }
 __device__ __forceinline__ void drop_store1(bf16_t* p, float x) { *reinterpret_cast<__bf16*>(p) = (__bf16)x; }
 
+// elements e0 .. e0 + EPL
 template <typename TX, typename TY>
-__global__ __launch_bounds__(256) void dropout_kernel(DropArgs<TX, TY> a) {
-  const uint64_t offset = a.offset + (a.more ? *a.more : 0);
-  const int64_t e0 = ((int64_t)blockIdx.x * 256 + threadIdx.x) * EPL;
-  if (e0 >= a.n) return;
+__device__ __forceinline__ void drop_piece(const DropArgs<TX, TY>& a, int64_t e0, uint64_t offset) {
   const bool whole = e0 + EPL <= a.n;
   float x[EPL], r[EPL];
   if (whole) {
@@ -87,6 +85,13 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropArgs<TX, TY> a) {
   }
 }
 
+template <typename TX, typename TY>
+__global__ __launch_bounds__(256) void dropout_kernel(DropArgs<TX, TY> a) {
+  const uint64_t offset = a.offset + (a.more ? *a.more : 0);
+  for (int64_t e0 = ((int64_t)blockIdx.x * 256 + threadIdx.x) * EPL; e0 < a.n; e0 += (int64_t)gridDim.x * (256 * EPL))
+    drop_piece(a, e0, offset);
+}
+
 gdr2_status drop_check(const gdr2_dropout* p, const uint64_t* more) {
   if (p == nullptr || p->n < 0 || !(p->p >= 0.0 && p->p < 1.0)) return GDR2_EINVAL;
   if (p->dtype != GDR2_BF16 && p->dtype != GDR2_FP32) return GDR2_EINVAL;
@@ -100,11 +105,12 @@ template <typename TX, typename TY>
 gdr2_status drop_launch(const gdr2_dropout* p, const uint64_t* more, const void* x, const void* r, void* y, hipStream_t st) {
   if (p->n == 0) return GDR2_OK;
   // round(p 2^32) is 2^32 for the last p below 1: all but the largest word are dropped then
-  const double least = std::floor(p->p * 4294967296.0 + 0.5);
+  const double least = std::nearbyint(p->p * 4294967296.0);
   const DropArgs<TX, TY> a{static_cast<const TX*>(x), static_cast<const TY*>(r), static_cast<TY*>(y), more, p->n, p->seed,
                            p->offset, least > 4294967295.0 ? 4294967295u : (uint32_t)least, (float)(1.0 / (1.0 - p->p))};
-  // at most 2^29 workgroups (n <= 2^40)
-  hipLaunchKernelGGL((dropout_kernel<TX, TY>), dim3((unsigned)((p->n + 256 * EPL - 1) / (256 * EPL))), dim3(256), 0, st, a);
+  // a launch has less than 2^32 threads: from 2^32 elements on a lane takes several pieces
+  const int64_t blocks = (p->n + 256 * EPL - 1) / (256 * EPL), most = 1 << 21;
+  hipLaunchKernelGGL((dropout_kernel<TX, TY>), dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, st, a);
   return hip_status(hipGetLastError(), st);
 }
 

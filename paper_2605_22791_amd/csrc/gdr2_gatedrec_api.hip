@@ -20,9 +20,11 @@ gdr2_status rec_check(const gdr2_gatedrec* p, const int32_t* cu, int nseq, bool 
   if (with_cu && nseq > 0 && (cu == nullptr || (reinterpret_cast<uintptr_t>(cu) & 3u) != 0)) return GDR2_EINVAL;
   if (p->D > kMaxChannels || nseq > kMaxSeqs) return GDR2_EUNSUPPORTED;
   if ((double)p->B * p->T >= 2147483648.0) return GDR2_EUNSUPPORTED;
-  // workgroups of one launch: (tile, 64 channels) and, token by token, (sequence, 256 channels)
-  if (((double)p->B * p->T / kRecBlock + 1) * ((p->D + 63) / 64) >= 2147483648.0) return GDR2_EUNSUPPORTED;
-  if ((double)(nseq > 0 ? nseq : p->B) * ((p->D + 255) / 256) >= 2147483648.0) return GDR2_EUNSUPPORTED;
+  // a launch has less than 2^32 threads: 512 for 64 tokens and 64 or 128 channels, and token by token
+  // 256 for a sequence and 256 channels
+  const double groups = (p->D + rec_channels(p->D) - 1) / rec_channels(p->D);
+  if (((double)p->B * p->T / kRecBlock + 1) * groups * (64 * kRecWaves) >= 4294967296.0) return GDR2_EUNSUPPORTED;
+  if ((double)(nseq > 0 ? nseq : p->B) * ((p->D + 255) / 256) * 256 >= 4294967296.0) return GDR2_EUNSUPPORTED;
   return GDR2_OK;
 }
 

@@ -49,7 +49,8 @@ def _rc(which, prob, cu=None, n=0, ptrs=None, ws_bytes=BIG):
 @pytest.mark.parametrize("which", ["fwd", "bwd", "step"])
 @pytest.mark.parametrize("kw,code", [
     (dict(B=0), EINVAL), (dict(T=0), EINVAL), (dict(D=-3), EINVAL), (dict(dtype=2), EINVAL), (dict(normalize=2), EINVAL),
-    (dict(D=65537), EUNSUPPORTED), (dict(B=1 << 16, T=1 << 15), EUNSUPPORTED)])
+    (dict(D=65537), EUNSUPPORTED), (dict(B=1 << 16, T=1 << 15), EUNSUPPORTED), (dict(B=1 << 15, T=1 << 15, D=1), EUNSUPPORTED),
+    (dict(B=1 << 10, T=1 << 17, D=1024), EUNSUPPORTED)])
 def test_recurrence_problem_checks(which, kw, code):
     assert _rc(which, _rec(**kw)) == code
     n = ctypes.c_size_t(0)
@@ -100,7 +101,7 @@ def _fc(which, prob, ptrs=None, ws_bytes=BIG):
 @pytest.mark.parametrize("kw,code", [
     (dict(rows=-1), EINVAL), (dict(D=0), EINVAL), (dict(F=-8), EINVAL), (dict(dtype=5), EINVAL), (dict(act=2), EINVAL),
     (dict(D=68), EUNSUPPORTED), (dict(F=4), EUNSUPPORTED), (dict(D=65544), EUNSUPPORTED),
-    (dict(rows=(1 << 24) + 1), EUNSUPPORTED)])
+    (dict(rows=(1 << 24) + 1), EUNSUPPORTED), (dict(rows=1 << 24, F=4096), EUNSUPPORTED)])
 def test_feed_forward_problem_checks(which, kw, code):
     assert _fc(which, _ff(**kw)) == code
     n = ctypes.c_size_t(0)
