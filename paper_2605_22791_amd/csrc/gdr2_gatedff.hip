@@ -112,19 +112,20 @@ struct FfTile {
   static constexpr int BNC = END == FF_GATE ? BN / 2 : BN;      // columns of N that a tile takes
 };
 
-// A wave's strip of C: 16 rows x WN columns, COLS of N; through LDS a lane has four neighbouring columns
-// of IT rows, RI apart.
+// A wave's strip of C: 16 rows x WN columns, COLS of N; through LDS a lane has CW neighbouring columns, 16
+// bytes of T, of IT rows, RI apart.
 template <typename T, int FORM, int END, int BM, int BN>
 struct FfStrip : FfTile<T, FORM, END, BM, BN> {
   using Z = FfTile<T, FORM, END, BM, BN>;
-  static constexpr int COLS = END == FF_GATE ? Z::WN / 2 : Z::WN, LR = COLS / 4, RI = 64 / LR, IT = 16 / RI;
+  static constexpr int CW = 16 / (int)sizeof(T), COLS = END == FF_GATE ? Z::WN / 2 : Z::WN;
+  static constexpr int LR = COLS / CW, RI = 64 / LR, IT = 16 / RI;
   static constexpr bool HALVES = END == FF_GATE && sizeof(T) == 2;
   static constexpr int NB = Z::WN / kFfBlock;                  // blocks of a row of the strip with a power of their own
   static_assert(!HALVES || COLS % kFfBlock == 0, "whole blocks");
   static constexpr int BYTES = 16 * (Z::SLD + (HALVES ? NB : 0)) * 4;  // LDS of a wave
   int64_t m, n;  // the strip's first row and column
   int r, c;      // the lane's first row and its columns, within the strip
-  __device__ __forceinline__ FfStrip(int64_t m, int64_t n, int lane) : m(m), n(n), r(lane / LR), c(4 * (lane % LR)) {}
+  __device__ __forceinline__ FfStrip(int64_t m, int64_t n, int lane) : m(m), n(n), r(lane / LR), c(CW * (lane % LR)) {}
   // the lane's rows that there are, RI apart
   __device__ __forceinline__ int rows(const FfArgs<T>& p) const {
     const int left = (int)min((int64_t)16, p.M - m) - r;
@@ -147,11 +148,14 @@ struct FfPast {
         u[it] = *reinterpret_cast<const f4*>(up);
       }
   }
-  __device__ __forceinline__ void get(int it, f4& gx, f4& ux) const { gx = g[it], ux = u[it]; }
+  __device__ __forceinline__ void get(int it, float (&gx)[4], float (&ux)[4]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) gx[i] = g[it][i], ux[i] = u[it][i];
+  }
 };
 template <class S>
 struct FfPast<bf16_t, S> {
-  f16x4 g[S::IT], u[S::IT];
+  f16x8 g[S::IT], u[S::IT];
   int8_t ge[S::IT], ue[S::IT];
   __device__ __forceinline__ void load(const FfArgs<bf16_t>& p, const S& s) {
     const int rows = s.rows(p);
@@ -161,25 +165,36 @@ struct FfPast<bf16_t, S> {
 #pragma unroll
     for (int it = 0; it < S::IT; ++it, gp += S::RI * p.N, up += S::RI * p.N, b += S::RI * nb)
       if (it < rows) {
-        g[it] = *reinterpret_cast<const f16x4*>(gp);
-        u[it] = *reinterpret_cast<const f16x4*>(up);
+        g[it] = *reinterpret_cast<const f16x8*>(gp);
+        u[it] = *reinterpret_cast<const f16x8*>(up);
         ge[it] = p.hid.ge[b];
         ue[it] = p.hid.ue[b];
       }
   }
-  __device__ __forceinline__ void get(int it, f4& gx, f4& ux) const {
+  __device__ __forceinline__ void get(int it, float (&gx)[8], float (&ux)[8]) const {
     const float a = ldexpf(1.f, -ge[it]), b = ldexpf(1.f, -ue[it]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) gx[i] = (float)g[it][i] * a, ux[i] = (float)u[it][i] * b;
+    for (int i = 0; i < 8; ++i) gx[i] = (float)g[it][i] * a, ux[i] = (float)u[it][i] * b;
   }
 };
 
-template <typename T>
-__device__ __forceinline__ void ff_put(T* to, const f4& x) {
-  if constexpr (sizeof(T) == 2)
-    st4(reinterpret_cast<__bf16*>(to), x[0], x[1], x[2], x[3]);
-  else
-    *reinterpret_cast<f4*>(to) = x;
+__device__ __forceinline__ void ff_put(float* to, const float (&x)[4]) { *reinterpret_cast<f4*>(to) = f4{x[0], x[1], x[2], x[3]}; }
+__device__ __forceinline__ void ff_put(bf16_t* to, const float (&x)[8]) { st8(reinterpret_cast<__bf16*>(to), round8(x)); }
+__device__ __forceinline__ void ff_keep(float* to, const float (&x)[4], float) { ff_put(to, x); }
+__device__ __forceinline__ void ff_keep(_Float16* to, const float (&x)[8], float f) {
+  f16x8 h;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) h[i] = (_Float16)(x[i] * f);
+  *reinterpret_cast<f16x8*>(to) = h;
+}
+template <int N>
+__device__ __forceinline__ void ff_take(const float* from, float (&x)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; i += 4) {
+    const f4 v = *reinterpret_cast<const f4*>(from + i);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[i + j] = v[j];
+  }
 }
 
 // act(g) and, where wanted, its slope
@@ -205,9 +220,9 @@ __device__ __forceinline__ void ff_wave_order() {
 }
 
 // A strip's products x, in the lanes' layout, through the wave's place in LDS (lds, BYTES of it).
-template <typename T, class S>
+template <typename T, int END, class S>
 __device__ __forceinline__ void ff_leave(const FfArgs<T>& p, const f4* x, float* lds, const S& s, const FfPast<T, S>* past,
-                                         int end, int lane) {
+                                         int lane) {
   float* power = lds + 16 * S::SLD;  // of the row's blocks: g's, then u's
   ff_wave_order();
 #pragma unroll
@@ -244,46 +259,41 @@ __device__ __forceinline__ void ff_leave(const FfArgs<T>& p, const f4* x, float*
   for (int it = 0; it < S::IT; ++it, at += S::RI * p.N) {
     if (it >= rows) continue;
     const int r = s.r + S::RI * it;
-    const f4 v = *reinterpret_cast<const f4*>(lds + r * S::SLD + s.c);
-    if (end == FF_STORE) {
+    float v[S::CW];
+    ff_take(lds + r * S::SLD + s.c, v);
+    if constexpr (END == FF_STORE) {
       ff_put((s.m + r < p.cut ? p.c[0] : p.c[1] - p.cut * p.N) + at, v);
-    } else if (end == FF_GATE) {
-      const f4 u = *reinterpret_cast<const f4*>(lds + r * S::SLD + S::COLS + s.c);
+    } else if constexpr (END == FF_GATE) {
+      using H = typename std::conditional<sizeof(T) == 2, _Float16, float>::type;
+      float u[S::CW];
+      ff_take(lds + r * S::SLD + S::COLS + s.c, u);
       if (p.hid.g) {
-        if constexpr (S::HALVES) {
-          const float fg = power[r * S::NB + s.c / kFfBlock], fu = power[r * S::NB + S::NB / 2 + s.c / kFfBlock];
-          *reinterpret_cast<f16x4*>(static_cast<_Float16*>(p.hid.g) + at) =
-              f16x4{(_Float16)(v[0] * fg), (_Float16)(v[1] * fg), (_Float16)(v[2] * fg), (_Float16)(v[3] * fg)};
-          *reinterpret_cast<f16x4*>(static_cast<_Float16*>(p.hid.u) + at) =
-              f16x4{(_Float16)(u[0] * fu), (_Float16)(u[1] * fu), (_Float16)(u[2] * fu), (_Float16)(u[3] * fu)};
-        } else {
-          *reinterpret_cast<f4*>(static_cast<float*>(p.hid.g) + at) = v;
-          *reinterpret_cast<f4*>(static_cast<float*>(p.hid.u) + at) = u;
-        }
+        const float* f = power + r * S::NB + s.c / kFfBlock;
+        ff_keep(static_cast<H*>(p.hid.g) + at, v, S::HALVES ? f[0] : 1.f);
+        ff_keep(static_cast<H*>(p.hid.u) + at, u, S::HALVES ? f[S::NB / 2] : 1.f);
       }
       if (p.h) {
-        f4 h;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < S::CW; ++i) {
           float a, slope;
           ff_act<false>(p.act, v[i], a, slope);
-          h[i] = a * u[i];
+          v[i] = a * u[i];
         }
-        ff_put(p.h + at, h);
+        ff_put(p.h + at, v);
       }
     } else {
-      f4 g, u, dg, du;
+      float g[S::CW], u[S::CW];
       past->get(it, g, u);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < S::CW; ++i) {
         float a, slope;
         ff_act<true>(p.act, g[i], a, slope);
-        dg[i] = v[i] * u[i] * slope;
-        du[i] = v[i] * a;
+        g[i] = v[i] * u[i] * slope;
+        u[i] = v[i] * a;
       }
       T* to = p.dgu + 2 * at - col;
-      ff_put(to, dg);
-      ff_put(to + p.N, du);
+      ff_put(to, g);
+      ff_put(to + p.N, u);
     }
   }
 }
@@ -444,11 +454,11 @@ __global__ __launch_bounds__(ff_threads(BM), 2) void ff_kernel(FfArgs<T> p) {
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       if (i + 1 < MT) past[(i + 1) & 1].load(p, strip(i + 1));
-      ff_leave<T, S>(p, acc[i], stage, strip(i), &past[i & 1], END, lane);
+      ff_leave<T, END, S>(p, acc[i], stage, strip(i), &past[i & 1], lane);
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < MT; ++i) ff_leave<T, S>(p, acc[i], stage, strip(i), nullptr, END, lane);
+    for (int i = 0; i < MT; ++i) ff_leave<T, END, S>(p, acc[i], stage, strip(i), nullptr, lane);
   }
 }
 
@@ -475,7 +485,7 @@ __global__ __launch_bounds__(256) void ff_join_kernel(FfArgs<T> p) {
   const S s((int64_t)im * BM + Z::WM * (wave / Z::NWN) + 16 * i, (int64_t)in * Z::BNC + S::COLS * (wave % Z::NWN), lane);
   FfPast<T, S> past;
   if constexpr (END == FF_GRAD) past.load(p, s);
-  ff_leave<T, S>(p, x, reinterpret_cast<float*>(stage[w4]), s, &past, END, lane);
+  ff_leave<T, END, S>(p, x, reinterpret_cast<float*>(stage[w4]), s, &past, lane);
 }
 
 // Few rows of A (up to 16 MT): the weights' way through memory is all there is.  A workgroup takes 16 rows of
