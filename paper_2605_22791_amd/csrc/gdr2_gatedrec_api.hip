@@ -37,13 +37,13 @@ struct RecLayout {
   } chain[2];  // forward, backward
   size_t states, total;
 };
-RecLayout rec_layout(const gdr2_gatedrec* p, bool bwd) {
+RecLayout rec_layout(const gdr2_gatedrec* p, int nseq, bool bwd) {
   RecLayout L{};
   const int64_t rows = (int64_t)p->B * p->T;
   size_t off = 0;
   for (int k = 0; k < (bwd ? 2 : 1); ++k) {
     RecLayout::Chain& c = L.chain[k];
-    const int tile = k == 0 ? rec_tile(rows, p->D) : kRecBlock;
+    const int tile = k == 0 ? rec_tile(nseq > 0 ? p->T / nseq : p->T, rows, p->D) : kRecBlock;
     c.tiles = (int)((rows + tile - 1) / tile);
     c.at = off;
     if (c.tiles > 1) {
@@ -114,7 +114,7 @@ gdr2_status gdr2_gatedrec_workspace_bytes(const gdr2_gatedrec* p, int32_t n_seqs
   if (bytes == nullptr) return GDR2_EINVAL;
   const gdr2_status s = rec_check(p, nullptr, n_seqs, false);
   if (s != GDR2_OK) return s;
-  *bytes = rec_layout(p, for_backward != 0).total;
+  *bytes = rec_layout(p, n_seqs, for_backward != 0).total;
   return GDR2_OK;
 }
 
@@ -124,7 +124,7 @@ gdr2_status gdr2_gatedrec_fwd(const gdr2_gatedrec* p, const int32_t* cu, int32_t
   const gdr2_status s = rec_check(p, cu, n, true);
   if (s != GDR2_OK) return s;
   if (!need(x) || !need(g) || !aligned16(i) || !aligned16(h0) || !need(o) || !aligned16(hT) || !need(ws)) return GDR2_EINVAL;
-  const RecLayout L = rec_layout(p, save != 0);
+  const RecLayout L = rec_layout(p, n, save != 0);
   if (ws_bytes < L.total) return GDR2_EWORKSPACE;
   hipError_t e = launch_rec_clear(rec_clear(ws, L.chain[0]), {}, stream);
   if (e == hipSuccess)
@@ -142,7 +142,7 @@ gdr2_status gdr2_gatedrec_bwd(const gdr2_gatedrec* p, const int32_t* cu, int32_t
       !aligned16(di) || !aligned16(dh0) || !need(ws))
     return GDR2_EINVAL;
   if ((i != nullptr) != (di != nullptr)) return GDR2_EINVAL;
-  const RecLayout L = rec_layout(p, true);
+  const RecLayout L = rec_layout(p, n, true);
   if (ws_bytes < L.total) return GDR2_EWORKSPACE;
   const auto run = [&](auto t) {
     using T = decltype(t);

@@ -95,7 +95,8 @@ def _check(B, T, D, dtype, seed=0, normalize=False, saved=False, **kw):
 
 @pytest.mark.parametrize("B,T,D", [(1, 1, 1), (2, 1, 64), (3, 5, 7), (4, 2, 300), (1, 63, 65), (2, 64, 130), (1, 65, 127),
                                    (3, 129, 512), (1, 511, 96), (2, 512, 128), (1, 513, 129), (2, 1000, 257), (7, 300, 66),
-                                   (1, 4099, 33), (5, 100, 1155), (1, 2048, 1024), (40, 33, 200)])
+                                   (1, 4099, 33), (5, 100, 1155), (1, 2048, 1024), (40, 33, 200),
+                                   (1, 20000, 33), (1, 30000, 200)])
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_shapes(B, T, D, dtype):
     _case(f"B {B} T {T} D {D} {dtype}")
@@ -122,7 +123,7 @@ def test_decays(shift, T):
 
 
 PACKED = [[1], [5, 1, 2], [0, 3, 0, 0, 4, 0], [64, 64, 64], [1] * 130, [300, 0, 17, 1, 1025, 63, 64, 65, 2, 511],
-          [2000, 1, 1, 1, 3000], [0, 0, 0], [7] * 200, [512, 512, 512, 512], [513, 511, 1, 1535]]
+          [2000, 1, 1, 1, 3000], [9000, 12000, 0, 700], [0, 0, 0], [7] * 200, [512, 512, 512, 512], [513, 511, 1, 1535]]
 
 
 @pytest.mark.parametrize("lengths", PACKED, ids=lambda x: f"{len(x)}x{sum(x)}")
