@@ -25,7 +25,8 @@
  * sequence passes h0 to h_T and dh_T to dh0.  A sequence's values never meet another's, NaN
  * and infinities neither.
  *
- * Errors, ownership, streams and GDR2_DEBUG_SYNC as in gdr2.h.  The same call gives the same bits.
+ * Errors, ownership, streams and GDR2_DEBUG_SYNC as in gdr2.h; calls that share a workspace have to follow
+ * one another (one stream, or an event between).  The same call gives the same bits.
  */
 #ifndef GDR2_GATEDREC_H_
 #define GDR2_GATEDREC_H_

@@ -34,6 +34,9 @@ namespace {
 
 constexpr uint32_t kNone = 0xffffffffu;
 constexpr uint32_t kCut = 1, kWait = 2;
+// Looks of 1 to 2 us before a tile gives up: seconds, where a wait takes some of them.  Only calls that
+// overlap on one workspace, which is not allowed, get there; their results are NaN, but they end.
+constexpr int kPatience = 1 << 22;
 
 // ---- CPL neighbouring channels of a lane, on their way from memory --------------------------
 template <typename T, int CPL>
@@ -217,7 +220,7 @@ __device__ __forceinline__ void rec_await(const RecChain& ch, int D, int k, int 
                                           RecLook<CPL, NW, BACK>& look, float (&h)[CPL]) {
   const int lane = threadIdx.x & 63;
   int seen = 0, from = -1, far = 0;
-  for (;;) {
+  for (int looks = 0; looks < kPatience; ++looks) {
     const int d = far * NW + wave;
     if (d < k && seen < 2) {
       const size_t at = (size_t)(k - 1 - d) * D + c;
@@ -263,8 +266,8 @@ __device__ __forceinline__ void rec_await(const RecChain& ch, int D, int k, int 
   }
   if (wave == 0) {
 #pragma unroll
-    for (int j = 0; j < CPL; ++j) h[j] = look.state[from][col + j];
-    for (int v = far * NW + from - 1; v >= 0; --v)
+    for (int j = 0; j < CPL; ++j) h[j] = from < 0 ? __uint_as_float(0x7fc00000u) : look.state[from][col + j];
+    for (int v = from < 0 ? -1 : far * NW + from - 1; v >= 0; --v)
 #pragma unroll
       for (int j = 0; j < CPL; ++j) {
         const float2 f = look.step[v][col + j];
@@ -299,6 +302,7 @@ __global__ __launch_bounds__(64 * kRecWaves, 4) void rec_fwd_kernel(RecArgs<T> a
   const int D = a.D, ncg = (D + 64 * CPL - 1) / (64 * CPL), tiles = (a.rows + TILE - 1) / TILE;
   int group;
   const int tile = rec_ticket(a.chain.ticket, ncg, tiles, group);
+  if ((uint32_t)tile >= (uint32_t)tiles) return;  // (a counter that another call's launch shares)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = CPL * lane, c = group * 64 * CPL + col;
   const bool on = c < D;
@@ -418,6 +422,7 @@ __global__ __launch_bounds__(64 * kRecWaves, 4) void rec_bwd_kernel(RecBwdArgs<T
   const int D = a.D, ncg = (D + 64 * CPL - 1) / (64 * CPL), tiles = (a.rows + TILE - 1) / TILE;
   int group;
   const int k = rec_ticket(a.chain.ticket, ncg, tiles, group), tile = tiles - 1 - k;
+  if ((uint32_t)k >= (uint32_t)tiles) return;  // (a counter that another call's launch shares)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = CPL * lane, c = group * 64 * CPL + col;
   const bool on = c < D;
