@@ -684,7 +684,10 @@ size_t ff_part_bytes(const FfArgs<T>& a) {
 template <typename T, int FORM, int END>
 hipError_t launch_ff(FfArgs<T> a, hipStream_t st) {
   if constexpr (FORM == FF_ROWS && END != FF_GRAD)
-    if (a.M <= 64 && !a.hid.g) {  // (a saving forward gives the bits of the backward's own g and u)
+    // Up to 64 rows; wide weights in bf16 up to 32, for every workgroup reads all of A.  A forward of 33, 48, 64
+    // rows: 4096 -> 11008 82, 95, 104 us, 85 in tiles; 2048 -> 5504 33, 36, 40, and 37; 1024 -> 2816 15 to 17, and
+    // 27; fp32 64 rows of 4096 -> 11008 263, and 349.  (A saving forward gives the bits of the backward's own g and u.)
+    if (a.M <= (sizeof(T) == 2 && a.N * a.K > 12000000 ? 32 : 64) && !a.hid.g) {
       if (a.M <= 16) return ff_thin<T, END, 1>(a, st);
       if (a.M <= 32) return ff_thin<T, END, 2>(a, st);
       return ff_thin<T, END, 4>(a, st);

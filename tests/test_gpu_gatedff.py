@@ -102,10 +102,11 @@ def test_options(dtype, act, saved):
 
 
 def test_larger_against_torch_in_64_bits():
-    """Enough tiles for every CU, partial ones at the ends; the reference on the GPU in 64 bits."""
+    """Enough tiles for every CU, partial ones at the ends; few rows of wide weights; the reference on the GPU in
+    64 bits."""
     import torch
     for rows, D, F, act in ((2100, 1048, 2840, "silu"), (4096, 1024, 2816, "gelu"), (700, 2048, 5504, "silu"),
-                              (4100, 2048, 5504, "gelu")):
+                              (4100, 2048, 5504, "gelu"), (32, 2048, 6000, "silu"), (33, 2048, 6000, "silu"), (64, 2048, 6000, "gelu")):
         _case(f"rows {rows} D {D} F {F}")
         gen = torch.Generator(device="cuda").manual_seed(rows)
         f = lambda *s: torch.randn(s, generator=gen, device="cuda")  # noqa: E731
