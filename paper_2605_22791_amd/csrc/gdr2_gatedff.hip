@@ -22,17 +22,12 @@
 // products.  A library's large bf16 product reaches 1.43 PFLOP/s on this card, and 1.26, 1.29 and 0.78 on the three
 // forms at this size.
 
-#include <algorithm>
-
 #include "gdr2_gatedff.hpp"
 #include "gdr2_bf16.hpp"
 
 namespace gdr2 {
 
 namespace {
-
-constexpr int kCUs = 256;
-constexpr int STEP = 128;  // bytes of a row that one step takes
 
 // 16 bytes of an operand: a bf16 fragment, or four fp32 ones
 template <typename T>
@@ -58,7 +53,7 @@ struct FfType<float> {
 // Rows: ROWS rows of 128 bytes, piece p of row r at place p ^ ff_row_swz(r).  16-byte reads serve 16 lanes
 // at a time: quads of rows {0-3, 8-11} or {4-7, 12-15}, two neighbouring pieces.
 __device__ __forceinline__ int ff_row_swz(int r) { return (r & 2) | ((r & 8) >> 1); }
-// Columns: STEP / E rows of ROWS elements.  bf16: the transposing load serves 32 lanes at a time, 32 bytes
+// Columns: kFfStep / E rows of ROWS elements.  bf16: the transposing load serves 32 lanes at a time, 32 bytes
 // of rows {0-3, 8-11} (+ 4); fp32: four rows, four apart, of 64 bytes.
 template <typename T, int RB>  // bytes of a row
 __device__ __forceinline__ int ff_col_swz(int k) {
@@ -69,8 +64,8 @@ __device__ __forceinline__ int ff_col_swz(int k) {
 // One operand's way into LDS: ROWS x 128 bytes by NW waves, 1 KB an instruction.
 template <typename T, bool COL, int ROWS, int NW>
 struct FfLoad {
-  static constexpr int NI = ROWS * STEP / 1024 / NW;             // instructions a wave
-  static constexpr int RB = COL ? ROWS * (int)sizeof(T) : STEP;  // bytes of an LDS row
+  static constexpr int NI = ROWS * kFfStep / 1024 / NW;             // instructions a wave
+  static constexpr int RB = COL ? ROWS * (int)sizeof(T) : kFfStep;  // bytes of an LDS row
   static constexpr int RI = 1024 / RB;                           // LDS rows an instruction
   // the exchange is the same in every instruction but for bit 3 of the row in fp32 columns
   static constexpr int FLIP = COL && sizeof(T) == 4 ? (NW * RI & 8) : 0;
@@ -104,17 +99,14 @@ constexpr unsigned kOutside = 0x80000000u;  // an offset past every buffer
 
 }  // namespace
 
-constexpr int ff_waves_m(int bm) { return bm == 64 ? 2 : bm / 64; }  // waves along M, two along N
-constexpr int ff_threads(int bm) { return 128 * ff_waves_m(bm); }
-
 template <typename T, int FORM, int END, int BM, int BN>
 struct FfTile {
   static constexpr int E = sizeof(T);
   static constexpr int NWM = ff_waves_m(BM), NWN = 2, NW = NWM * NWN, WM = BM / NWM;  // waves of WM x WN
   static constexpr int WN = BN / NWN, MT = WM / 16, NT = WN / 16;
-  static constexpr int BK = STEP / E;
+  static constexpr int BK = kFfStep / E;
   static constexpr bool ACOL = FORM == FF_COLUMNS, BCOL = FORM != FF_ROWS;
-  static constexpr int BUF = (BM + BN) * STEP;
+  static constexpr int BUF = (BM + BN) * kFfStep;
   static constexpr int SLD = WN + 4;                            // floats from row to row where C passes through LDS
   static constexpr int BNC = END == FF_GATE ? BN / 2 : BN;      // columns of N that a tile takes
 };
@@ -369,7 +361,7 @@ __global__ __launch_bounds__(ff_threads(BM), 2) void ff_kernel(FfArgs<T> p) {
     }
     {
       const bool past = !Z::BCOL && last && k0 + fb.piece * (16 / E) >= p.K;
-      to += BM * STEP;
+      to += BM * kFfStep;
       if constexpr (END == FF_GATE) {
         // the tile's rows: for each wave column half of them Wg's, half Wu's, of the same channels
         constexpr int HALF = Z::WN / 2;
@@ -395,7 +387,7 @@ __global__ __launch_bounds__(ff_threads(BM), 2) void ff_kernel(FfArgs<T> p) {
   };
   // fragment of 16 rows (of M or N) from r0, half ks of the step
   const auto rows_frag = [&](const unsigned char* s, int r0, int ks) {
-    return *reinterpret_cast<const Frag*>(s + (r0 + r16) * STEP + (((4 * ks + grp) ^ ff_row_swz(r16)) << 4));
+    return *reinterpret_cast<const Frag*>(s + (r0 + r16) * kFfStep + (((4 * ks + grp) ^ ff_row_swz(r16)) << 4));
   };
   const auto cols_frag = [&](const unsigned char* s, auto row_bytes, int r0, int ks) {
     constexpr int RB = decltype(row_bytes)::value;
@@ -423,7 +415,7 @@ __global__ __launch_bounds__(ff_threads(BM), 2) void ff_kernel(FfArgs<T> p) {
     ff_landed();
     __syncthreads();
     if (s + 1 < s1) fetch(s + 1);
-    const unsigned char *sa = smem + (s & 1) * Z::BUF, *sb = sa + BM * STEP;
+    const unsigned char *sa = smem + (s & 1) * Z::BUF, *sb = sa + BM * kFfStep;
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
       Frag a[MT], b[NT];
@@ -595,59 +587,6 @@ __global__ __launch_bounds__(512) void ff_thin_kernel(FfArgs<T> p) {
 
 namespace {
 
-// How a call is laid out: the tile size and what the tiles left over are cut into, by the time that they
-// would take, in us: rounds of as many tiles as there are places, a part of a round for those that are
-// cut, and parts' way through memory and a launch.  Rates measured: 256 x 256 tiles 1.2 PFLOP/s in bf16, 128 x 128
-// 1.0, 64 x 64 (four a CU; FF_GATE: 64 x 128) 0.6; in fp32 0.1 either way.  Against each size by itself, 18 bf16
-// and 7 fp32 problems of 64 to 16000 rows, the choice was the best or within 9 % of it, both ways.
-struct FfPlan {
-  int bm, bn, slots;
-  int tm[2], tn[2], tiles, full, split;
-  double us;
-};
-// sizes of one or two products with the same sum
-struct FfSize {
-  int64_t M[2], N[2], K;
-  int pairs;
-};
-FfPlan ff_plan(int end, const FfSize& z, int E, int bm, int bn, int a_cu, double rate) {
-  FfPlan q{};
-  q.bm = bm;
-  q.bn = bn;
-  q.slots = a_cu * kCUs;
-  int64_t tiles = 0;
-  for (int k = 0; k < 2; ++k) {
-    const int bnc = end == FF_GATE ? bn / 2 : bn;
-    q.tm[k] = (int)((z.M[k] + bm - 1) / bm);
-    q.tn[k] = (int)((z.N[k] + bnc - 1) / bnc);
-    tiles += (int64_t)q.tm[k] * q.tn[k];
-  }
-  q.tiles = (int)tiles;
-  const int64_t steps = (z.K + STEP / E - 1) / (STEP / E) * z.pairs, left = tiles % q.slots;
-  const double tile = 2e-9 * bm * bn * (double)(steps * (STEP / E)) / (rate / q.slots);  // us; rate in PFLOP/s
-  q.full = q.tiles;
-  q.split = 1;
-  q.us = tile * (double)((tiles + q.slots - 1) / q.slots);
-  for (int64_t split = 2; left > 0 && split <= q.slots / left && split <= steps / 4; ++split) {
-    const double us = tile * ((double)(tiles / q.slots) + 1.0 / split) + 4.0 + (double)left * split * bm * bn * 8.0 / 4.8e6;
-    if (us < q.us) {
-      q.us = us;
-      q.split = (int)split;
-      q.full = (int)(tiles - left);
-    }
-  }
-  return q;
-}
-FfPlan ff_choose(int end, const FfSize& z, int E) {
-  const FfPlan mid = ff_plan(end, z, E, 128, 128, 2, E == 2 ? 1.0 : 0.1);
-  const FfPlan small = ff_plan(end, z, E, 64, E == 2 && end == FF_GATE ? 128 : 64, 4, E == 2 ? 0.6 : 0.1);
-  const FfPlan& best = small.us < mid.us ? small : mid;
-  if (E == 4) return best;
-  const FfPlan large = ff_plan(end, z, E, 256, 256, 1, 1.2);
-  return best.us < large.us ? best : large;
-}
-size_t ff_part_bytes(const FfPlan& q) { return (size_t)(q.tiles - q.full) * q.split * q.bm * q.bn * 4; }
-
 template <typename T>
 FfSize ff_size(const FfArgs<T>& a) {
   return {{a.M, a.also.M}, {a.N, a.also.N}, a.K, a.pairs};
@@ -684,10 +623,7 @@ size_t ff_part_bytes(const FfArgs<T>& a) {
 template <typename T, int FORM, int END>
 hipError_t launch_ff(FfArgs<T> a, hipStream_t st) {
   if constexpr (FORM == FF_ROWS && END != FF_GRAD)
-    // Up to 64 rows; wide weights in bf16 up to 32, for every workgroup reads all of A.  A forward of 33, 48, 64
-    // rows: 4096 -> 11008 82, 95, 104 us, 85 in tiles; 2048 -> 5504 33, 36, 40, and 37; 1024 -> 2816 15 to 17, and
-    // 27; fp32 64 rows of 4096 -> 11008 263, and 349.  (A saving forward gives the bits of the backward's own g and u.)
-    if (a.M <= (sizeof(T) == 2 && a.N * a.K > 12000000 ? 32 : 64) && !a.hid.g) {
+    if (ff_thin_rows(a.M, a.N, a.K, sizeof(T)) && !a.hid.g) {
       if (a.M <= 16) return ff_thin<T, END, 1>(a, st);
       if (a.M <= 32) return ff_thin<T, END, 2>(a, st);
       return ff_thin<T, END, 4>(a, st);

@@ -2,21 +2,10 @@
 // the kernels.
 #pragma once
 
+#include "gdr2_gatedff_plan.hpp"
 #include "gdr2_kernels.hpp"
 
 namespace gdr2 {
-
-// Products C = A B, A (M, K), B (K, N), fp32 accumulation.  An operand lies with its sum along the rows
-// of memory ("rows") or across them ("columns"):
-//     FF_ROWS     A (M, K), B^T (N, K)     x Wg^T, x Wu^T, h Wd^T
-//     FF_MIXED    A (M, K), B (K, N)       dy Wd, dg Wg + du Wu
-//     FF_COLUMNS  A^T (K, M), B (K, N)     dg^T x, du^T x, dy^T h
-enum FfForm : int { FF_ROWS = 0, FF_MIXED = 1, FF_COLUMNS = 2 };
-// What becomes of C:
-//     FF_STORE  rounded and stored
-//     FF_GATE   B is a pair, C a pair g, u: h = act(g) u, and g, u themselves where asked for
-//     FF_GRAD   C is dh: dg and du from it and the stored g, u
-enum FfEnd : int { FF_STORE = 0, FF_GATE = 1, FF_GRAD = 2 };
 
 // g and u on their way from the forward to the backward, (M, N): fp32 problems as they are; bf16 ones in
 // fp16, with a power of two for every row and 32 channels that takes their largest finite magnitude to

@@ -22,7 +22,7 @@ gdr2_status ff_check(const gdr2_gatedff* p) {
   if (p->dtype != GDR2_BF16 && p->dtype != GDR2_FP32) return GDR2_EINVAL;
   if (p->act != GDR2_ACT_SILU && p->act != GDR2_ACT_GELU) return GDR2_EINVAL;
   if (p->D % 8 != 0 || p->F % 8 != 0 || p->D > kMaxWidth || p->F > kMaxWidth || p->rows > kMaxRows) return GDR2_EUNSUPPORTED;
-  // a launch has less than 2^32 threads; a tile of 64 x 64 takes 256
+  // a launch has less than 2^32 threads: ff_plan has tiles for every call within these
   if ((double)p->rows * std::max(p->D, p->F) >= 68719476736.0) return GDR2_EUNSUPPORTED;  // 2^36 values
   return GDR2_OK;
 }
