@@ -663,16 +663,17 @@ hipError_t launch_rec_fwd(const RecArgs<T>& a, hipStream_t st) {
     constexpr bool G = decltype(gated)::value, N = decltype(norm)::value;
     constexpr int R = kRecTile / kRecWaves;
     const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a); };
+    // (a far look goes with tiles of kRecTile)
     if (rec_channels(a.D) == 128) {
-      if (tile == kRecTile)
-        far ? go(rec_fwd_kernel<T, 2, R, kRecFar / 2, G, N>) : go(rec_fwd_kernel<T, 2, R, 1, G, N>);
+      if (far)
+        go(rec_fwd_kernel<T, 2, R, kRecFar / 2, G, N>);
       else
-        far ? go(rec_fwd_kernel<T, 2, R / 2, kRecFar / 2, G, N>) : go(rec_fwd_kernel<T, 2, R / 2, 1, G, N>);
+        tile == kRecTile ? go(rec_fwd_kernel<T, 2, R, 1, G, N>) : go(rec_fwd_kernel<T, 2, R / 2, 1, G, N>);
     } else {
-      if (tile == kRecTile)
-        far ? go(rec_fwd_kernel<T, 1, R, kRecFar, G, N>) : go(rec_fwd_kernel<T, 1, R, 1, G, N>);
+      if (far)
+        go(rec_fwd_kernel<T, 1, R, kRecFar, G, N>);
       else
-        far ? go(rec_fwd_kernel<T, 1, R / 2, kRecFar, G, N>) : go(rec_fwd_kernel<T, 1, R / 2, 1, G, N>);
+        tile == kRecTile ? go(rec_fwd_kernel<T, 1, R, 1, G, N>) : go(rec_fwd_kernel<T, 1, R / 2, 1, G, N>);
     }
     return hipGetLastError();
   });
