@@ -67,3 +67,29 @@ def test_every_launch_of_the_documented_range_has_less_than_2_32_threads(shim):
             for E in (2, 4):
                 threads = plan(shim, p, E)[-1]
                 assert threads < 1 << 32, (rows, D, F, name, E, threads)
+
+
+def _combinations(shim, rows, D, F, E):
+    """The forms of the product kernel that a problem runs: (bytes of a value, product, tile, whole or cut)"""
+    out = set()
+    for name, p in products(rows, D, F).items():
+        tile, _, tiles, whole, _, _ = plan(shim, p, E)
+        out |= {(E, name, tile, "whole")} if whole else set()
+        out |= {(E, name, tile, "cut")} if whole < tiles else set()
+    return out
+
+
+def test_the_gpu_tests_have_every_tile_that_is_chosen(shim):
+    from tests.test_gpu_gatedff_sizes import SHAPES
+    r = random.Random(2)
+    spread = lambda lo, hi: int(lo * (hi / lo) ** r.random())  # noqa: E731
+    found = {E: set() for E in (2, 4)}
+    for _ in range(60000):
+        rows, D, F = spread(1, 1 << 18), spread(1, 8192) * 8, spread(1, 8192) * 8
+        if rows * max(D, F) < 1 << 36:
+            E = r.choice((2, 4))
+            found[E] |= _combinations(shim, rows, D, F, E)
+    for dtype, E in (("bf16", 2), ("fp32", 4)):
+        tested = set().union(*(_combinations(shim, rows, D, F, E) for rows, D, F, t, _ in SHAPES if t == dtype))
+        assert not found[E] - tested, found[E] - tested
+    assert len(found[2]) == 30 and len(found[4]) == 20  # five products, three tiles or two, whole and cut
