@@ -71,6 +71,16 @@ class FeedForward(torch.autograd.Function):
         return d["dx"], d["dw_gate"], d["dw_up"], d["dw_down"]
 
 
+def recurrence(v, g, i, h0):
+    """o, h_T; nothing is kept where no gradient will be asked for."""
+    return Recurrence.apply(v, g, i, h0) if torch.is_grad_enabled() else g2.gdr2_gatedrec_fwd(v, g, i, h0, normalize=True)
+
+
+def feed_forward(n, w_gate, w_up, w_down):
+    """Decoding, a call that keeps nothing: few rows then take the kernels made for them."""
+    return (FeedForward.apply if torch.is_grad_enabled() else g2.gdr2_gatedff_fwd)(n, w_gate, w_up, w_down)
+
+
 class Dropout(torch.autograd.Function):
     """residual + dropout(y); the backward forms the mask again from the seed and the offset."""
 
@@ -107,13 +117,13 @@ class Layer(torch.nn.Module):
         if step:
             o = g2.gdr2_gatedrec_step(v, g, i, h, normalize=True)
         else:
-            o, h = Recurrence.apply(v, g, i, h)
+            o, h = recurrence(v, g, i, h)
         a, _ = BlockNorm.apply(o, None, z, None, None, None)
         p, seed, number = drop
         at = (number << 16) + 2 * self.site  # an offset of its own for each dropout of each pass
         x = Dropout.apply(a @ self.w_out.t().to(dt), x, p, seed, at)
         _, n = BlockNorm.apply(x, None, None, None, None, self.w_mid)
-        y = FeedForward.apply(n.to(dt), self.w_gate.to(dt), self.w_up.to(dt), self.w_down.to(dt))
+        y = feed_forward(n.to(dt), self.w_gate.to(dt), self.w_up.to(dt), self.w_down.to(dt))
         x = Dropout.apply(y, x, p, seed, at + 1)
         _, n = BlockNorm.apply(x, None, None, None, None, self.w_next)
         return n.to(dt), x, h
