@@ -6,7 +6,8 @@ keep comes from a counter-based generator (Philox 4x32, ten rounds) by the eleme
 memory, the seed and the offset, each 64 bits, and is never stored: the backward forms it
 again.  x is bfloat16 or float32; residual and y share a type, that of x or float32.  offset
 is an int, or an int64 device tensor of one element that the kernel reads when it runs, so that a
-captured call can drop other elements on every replay.
+captured call can drop other elements on every replay.  more is such a tensor too, added to an offset that
+is an int (modulo 2^64): the dropouts of a captured step share one counter and have an offset each.
 """
 
 import ctypes
@@ -31,21 +32,24 @@ def _declare(L):
         f.restype = ctypes.c_int
 
 
-def _problem(t, p, seed, offset, code, stream):
+def _problem(t, p, seed, offset, more, code, stream):
     """The problem and the device part of the offset (or None)."""
     torch = _torch()
     if not 0.0 <= p < 1.0:
         raise ValueError(f"p: {p}, expected 0 <= p < 1")
-    more = None
+    name = "more"
     if isinstance(offset, torch.Tensor):
-        _require("offset", offset, offset.shape, torch.int64, t.device)
-        if offset.numel() != 1:
-            raise ValueError("offset: expected an int or an int64 device tensor of one element")
-        more, offset = offset, 0
+        if more is not None:
+            raise ValueError("more: beside an offset that is a tensor itself")
+        name, more, offset = "offset", offset, 0
+    if more is not None:
+        _require(name, more, more.shape, torch.int64, t.device)
+        if more.numel() != 1:
+            raise ValueError(f"{name}: expected an int64 device tensor of one element")
     return Gdr2Dropout(t.numel(), float(p), int(seed) & _M64, int(offset) & _M64, code, stream), more
 
 
-def gdr2_dropout_fwd(x, p, seed, *, offset=0, residual=None, y=None):
+def gdr2_dropout_fwd(x, p, seed, *, offset=0, more=None, residual=None, y=None):
     """Returns y, of the type of the residual (of x without one).  y may be the residual, or x of that type."""
     torch = _torch()
     code, dev = _dtype_code(x), x.device
@@ -56,7 +60,7 @@ def gdr2_dropout_fwd(x, p, seed, *, offset=0, residual=None, y=None):
         if stream != x.dtype and stream != torch.float32:
             raise TypeError(f"residual: {stream}, expected {x.dtype} or torch.float32")
         _require("residual", residual, x.shape, stream, dev)
-    prob, more = _problem(x, p, seed, offset, code, GDR2_FP32 if stream is torch.float32 else GDR2_BF16)
+    prob, more = _problem(x, p, seed, offset, more, code, GDR2_FP32 if stream is torch.float32 else GDR2_BF16)
     if y is None:
         y = torch.empty_like(x, dtype=stream)
     else:
@@ -69,7 +73,7 @@ def gdr2_dropout_fwd(x, p, seed, *, offset=0, residual=None, y=None):
     return y
 
 
-def gdr2_dropout_bwd(dy, p, seed, *, offset=0, dtype=None, dx=None):
+def gdr2_dropout_bwd(dy, p, seed, *, offset=0, more=None, dtype=None, dx=None):
     """Returns dx, the gradient at x, in `dtype` (that of x; None: that of dy).  The residual's gradient is dy."""
     torch = _torch()
     code = _dtype_code(dy)
@@ -78,7 +82,7 @@ def gdr2_dropout_bwd(dy, p, seed, *, offset=0, dtype=None, dx=None):
         dtype = dy.dtype if dx is None else dx.dtype
     if dtype != dy.dtype and (dtype, dy.dtype) != (torch.bfloat16, torch.float32):
         raise TypeError(f"dtype: {dtype} beside a gradient in {dy.dtype}")
-    prob, more = _problem(dy, p, seed, offset, GDR2_FP32 if dtype is torch.float32 else GDR2_BF16, code)
+    prob, more = _problem(dy, p, seed, offset, more, GDR2_FP32 if dtype is torch.float32 else GDR2_BF16, code)
     if dx is None:
         dx = torch.empty_like(dy, dtype=dtype)
     else:
