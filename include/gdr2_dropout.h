@@ -6,7 +6,7 @@
  *     dx_e = k_e dy_e / (1 - p)              (r's gradient is dy itself)
  *
  * k_e is 1 where word e of a counter-based generator is at least p 2^32 (rounded to a whole number,
- * halves to even), else 0, and is formed again where it is needed: no mask is stored.  Words are
+ * halves to even, and 2^32 - 1 at most), else 0, and is formed again where it is needed: no mask is stored.  Words are
  * those of Philox 4x32 with ten rounds (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as
  * easy as 1, 2, 3", SC 2011): word e is word e % 4 of the block with counter (e / 4, offset), each
  * 64 bits, low half first, and key `seed`.  Calls with the same seed and offset drop the same

@@ -15,9 +15,10 @@
  *     x, i, o, dout, dx, di   (B, T, D)   problem->dtype (bf16 or fp32)
  *     g, dg                   (B, T, D)   fp32
  *     h0, h_T, h, dh_T, dh0   (B, D), packed (n_seqs, D)   fp32
- * Any D from 1 to 65536; up to 2^31 - 1 tokens (B T), and up to 2^23 workgroups, which take 64 tokens
- * of 128 channels each (64 where D is odd or at most 64), else GDR2_EUNSUPPORTED.  States are fp32
- * throughout; o and the gradients are rounded once.
+ * Any D from 1 to 65536, and fewer than 2^23 workgroups, which take 64 tokens of 128 channels each (64
+ * where D is odd or at most 64): fewer than 2^29 tokens (B T) of up to 64 channels, 2^25 of 2048.  Up to 2^24 packed
+ * sequences, and fewer than 2^32 states with D rounded up to 256.  Else GDR2_EUNSUPPORTED, token by
+ * token too.  States are fp32 throughout; o and the gradients are rounded once.
  *
  * Packed batches (B = 1, n_seqs > 0): cu_seqlens (n_seqs + 1) holds the sequences' offsets,
  * 0 <= cu_seqlens[0] <= ... <= cu_seqlens[n_seqs] <= T; n_seqs = 0: fixed length, cu_seqlens
@@ -26,7 +27,8 @@
  * and infinities neither.
  *
  * Errors, ownership, streams and GDR2_DEBUG_SYNC as in gdr2.h; calls that share a workspace have to follow
- * one another (one stream, or an event between).  The same call gives the same bits.
+ * one another (one stream, or an event between).  Calls that overlap on one end, but their outputs are
+ * unspecified: wrong, unwritten or NaN.  The same call gives the same bits.
  */
 #ifndef GDR2_GATEDREC_H_
 #define GDR2_GATEDREC_H_

@@ -29,7 +29,8 @@ constexpr int ff_threads(int bm) { return 128 * ff_waves_m(bm); }
 // How a call is laid out: the tile size and what the tiles left over are cut into, by the time that they
 // would take, in us: rounds of as many tiles as there are places, a part of a round for those that are
 // cut, and parts' way through memory and a launch.  Rates measured: 256 x 256 tiles 1.2 PFLOP/s in bf16, 128 x 128
-// 1.0, 64 x 64 (four a CU; FF_GATE: 64 x 128) 0.6; in fp32 0.1 either way.  Against each size by itself, 18 bf16
+// 1.0, 64 x 64 (FF_GATE: 64 x 128) 0.6; in fp32 0.1 either way.  Places are taken as one, two and four a
+// CU; registers and LDS have room for one, two, and five of 64 x 64, three of 64 x 128.  Against each size by itself, 18 bf16
 // and 7 fp32 problems of 64 to 16000 rows, the choice was the best or within 9 % of it, both ways.
 struct FfPlan {
   int bm, bn, slots;
@@ -83,8 +84,9 @@ inline FfPlan ff_choose(int end, const FfSize& z, int E) {
 inline size_t ff_part_bytes(const FfPlan& q) { return (size_t)(q.tiles - q.full) * q.split * q.bm * q.bn * 4; }
 
 // Up to 64 rows; wide weights in bf16 up to 32, for every workgroup reads all of A.  A forward of 33, 48, 64
-// rows: 4096 -> 11008 82, 95, 104 us, 85 in tiles; 2048 -> 5504 33, 36, 40, and 37; 1024 -> 2816 15 to 17, and
-// 27; fp32 64 rows of 4096 -> 11008 263, and 349.  (A saving forward gives the bits of the backward's own g and u.)
+// rows: 4096 -> 11008 (45 M weights) 82, 95, 104 us, 85 in tiles; 2048 -> 5504 (11 M) 33, 36, 40, and 37; 1024 -> 2816
+// 15 to 17, and 27.  Nothing between 11 M and 45 M was measured; the bound keeps 2048 -> 5504 whole, which gains up to 48
+// rows and loses 3 us at 64.  fp32 64 rows of 4096 -> 11008 263, and 349.  (A saving forward gives the bits of the backward's own g and u.)
 inline bool ff_thin_rows(int64_t M, int64_t N, int64_t K, int E) { return M <= (E == 2 && N * K > 12000000 ? 32 : 64); }
 
 }  // namespace gdr2

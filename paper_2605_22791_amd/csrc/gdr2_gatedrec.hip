@@ -4,8 +4,8 @@
 // bound by memory: the forward reads x, i and g and writes o, 10 bytes an element in bf16, the
 // backward reads do besides and writes three gradients, 18.
 //
-// A workgroup takes a tile of 128 tokens and 64 or 128 channels, each wave R of the tokens in
-// registers, a lane one or two channels.  A step is affine in the state, so a wave's tokens are one
+// A workgroup takes a tile of 128 or 64 tokens (the backward: 64) and 64 or 128 channels, each wave R of the
+// tokens in registers, a lane one or two channels.  A step is affine in the state, so a wave's tokens are one
 // factor and one addend; waves meet in LDS, tiles through memory: a tile publishes its factor and
 // addend, then waits for the state before it, which it takes from the nearest of the eight tiles
 // before (each wave looks at one; on long chains up to 128 of them) that has published its own, folded with
@@ -14,9 +14,9 @@
 // memory, about 1.5 us.  The backward does the same from the other end, with the states before the
 // tiles as a forward left them.
 //
-// Measured (normalized, input gate, bf16): 8 x 4096 tokens of 2048 channels forward 162 us (671 MB, 4.1
-// TB/s), backward 275 us (1.2 GB, 4.4 TB/s); 65536 tokens of 2048 without gate and norm 243 and 443 us (4.4 and
-// 4.2 TB/s).  Below that: 1000 tokens of 2048 channels 15 and 20 us, the latency of a tile's life.
+// Measured (normalized, input gate, bf16; medians of ten traced calls): 8 x 4096 tokens of 2048 channels forward
+// 161 us (671 MB, 4.2 TB/s), backward 283 us (1.2 GB, 4.3 TB/s); 65536 tokens of 2048 without gate and norm 245
+// and 461 us (1.07 GB, 4.4 TB/s, and 1.88 GB, 4.1 TB/s).  Below that: 1000 tokens of 2048 channels 15 and 20 us, the latency of a tile's life.
 //
 // Nobody waits for a tile that has not begun: tiles are taken by a counter, in the order of the
 // chain, and a tile's predecessors have smaller numbers.  A published value is a whole word that is
@@ -34,8 +34,9 @@ namespace {
 
 constexpr uint32_t kNone = 0xffffffffu;
 constexpr uint32_t kCut = 1, kWait = 2;
-// Looks of 1 to 2 us before a tile gives up: seconds, where a wait takes some of them.  Only calls that
-// overlap on one workspace, which is not allowed, get there; their results are NaN, but they end.
+// Looks of 1 to 2 us before a tile gives up: seconds, where a wait takes some of them.  Only calls that overlap on
+// one workspace, which is not allowed, get there.  They end, and no more than that is ensured: a tile that gives up
+// takes NaN, one whose ticket is out of range writes nothing, and one may fold in what the other call published.
 constexpr int kPatience = 1 << 22;
 
 // ---- CPL neighbouring channels of a lane, on their way from memory --------------------------
